@@ -482,6 +482,106 @@ lightkv_status lightkv_compress_schedule_ratio(const lightkv_stage *stages, int3
                                                float softmax_scale, void *ws, size_t ws_bytes,
                                                int32_t *h_cu_vis_out, void *stream);
 
+/* ---- The cache behind the step: pages, their tables, and the attention of decoded tokens ------------------------------
+ *
+ * A compressed layer leaves every sequence with fewer K/V rows than it had tokens, and how many may be known on the device
+ * only (cu_vis_out).  The calls below keep such rows in pages of equal size: lightkv_page_alloc hands pages to the sequences
+ * and says where every new row goes, lightkv_page_write puts the rows there, lightkv_page_attention is the attention of one
+ * new token per sequence over what its pages hold, lightkv_page_free takes pages back.  None of them needs a length on the
+ * host, so a decoding loop can be captured into a graph and replayed while the sequences grow.
+ *
+ * Keys and values of a layer are a pool of n_pages pages of page_tokens rows of [kv_heads, head_dim]: element e of head h of
+ * row t of page i sits at K[i*k_page_stride + t*k_tok_stride + h*k_head_stride + e], V alike, so rows may be token-major
+ * inside a page (as the rest of this header has them) or head-major.  Sequence b owns the pages table[b*table_stride + j],
+ * j < ceil(seq_lens[b] / page_tokens), its token t is row t % page_tokens of page j = t / page_tokens; entries behind
+ * these are not looked at.  One table may serve the pools of several layers.
+ */
+#define LIGHTKV_PAGED_MAX_BATCH 4096   /* sequences in one call  */
+
+typedef struct lightkv_pages {
+  int32_t batch;              /* sequences, = rows of the table; 1 .. LIGHTKV_PAGED_MAX_BATCH                   */
+  int32_t n_pages;            /* pages of the pool; n_pages * page_tokens < 2^31                                */
+  int32_t page_tokens;        /* rows of a page: a power of two from 8 to 1024                                  */
+  int32_t max_pages;          /* entries of a table row; max_pages * page_tokens < 2^31                         */
+  int64_t table_stride;       /* ints from one row of the table to the next, >= max_pages                       */
+  int32_t *table;             /* device                                                                         */
+  /* the rest is used by lightkv_page_write and lightkv_page_attention only                                     */
+  int32_t heads, kv_heads;    /* query heads, a multiple of kv_heads: query head h reads K/V head h / (heads / kv_heads) */
+  int32_t head_dim;           /* 32, 64 or 128                                                                  */
+  int32_t dtype;              /* lightkv_dtype of K, V, and of rows, queries and outputs                        */
+  void *K, *V;                /* device, the pools                                                              */
+  int64_t k_page_stride, k_tok_stride, k_head_stride;   /* elements, not negative                               */
+  int64_t v_page_stride, v_tok_stride, v_head_stride;
+} lightkv_pages;
+
+/*
+ * Pages and slots for new tokens.  Sequence b holds seq_lens[b] tokens and gets new_b = cu_new[b+1] - cu_new[b] more (cu_new:
+ * device [batch+1], e.g. cu_vis_out, cu_txt, or 0, 1, 2, .. for a decoded token each).  free_pages[0 .. free_count[0]) is a
+ * stack of the pages nobody owns (device; free_pages has n_pages entries).
+ *   need_b = ceil((seq_lens[b] + new_b) / page_tokens) - ceil(seq_lens[b] / page_tokens) pages are asked for in the order of
+ *   b; a sequence is refused if its need is above zero and the pages asked for up to and with it are more than free_count[0]
+ *   (what was refused keeps its place in the order: later sequences are served only if they need no page).  The i-th page
+ *   that is asked for is free_pages[free_count[0] - 1 - i].
+ * Outputs (device):
+ *   table            the new pages, behind those the sequence has; all other entries stay
+ *   slots            row t in [cu_new[b], cu_new[b+1]): page * page_tokens + row in the page, of the token at position
+ *                    seq_lens[b] + t - cu_new[b]; -1 if the sequence was refused (or the page number is none of the pool's).
+ *                    slots has slot_rows entries; those no sequence owns stay as they were
+ *   seq_lens_out     [batch] seq_lens[b] + new_b; seq_lens[b] if refused.  May be the array seq_lens itself
+ *   free_count_out   [1] pages that are left.  May be free_count itself.  free_pages is only read
+ *   status           [batch], may be NULL: 0; 1 where the pool ran short; 2 where the tokens do not fit the table row or
+ *                    slots, or offsets or lengths are impossible (refused without a place in the order)
+ */
+lightkv_status lightkv_page_alloc(const lightkv_pages *p, const int32_t *cu_new, const int32_t *seq_lens,
+                                  const int32_t *free_pages, const int32_t *free_count, int32_t *seq_lens_out,
+                                  int32_t *free_count_out, int32_t *slots, int64_t slot_rows, int32_t *status,
+                                  void *stream);
+
+/*
+ * Takes back the pages of every sequence with done[b] != 0 (device [batch]): its ceil(seq_lens[b] / page_tokens) table entries
+ * are put on the stack, sequences in the order of b, entries of a sequence in the order of its row.
+ *   free_pages       [n_pages] in and out: entries from free_count[0] on are written
+ *   seq_lens_out     [batch] 0 where done, seq_lens[b] elsewhere.  May be seq_lens itself
+ *   free_count_out   [1] may be free_count itself; never more than n_pages (what would not fit the stack is dropped)
+ */
+lightkv_status lightkv_page_free(const lightkv_pages *p, const int32_t *done, const int32_t *seq_lens, int32_t *free_pages,
+                                 const int32_t *free_count, int32_t *seq_lens_out, int32_t *free_count_out, void *stream);
+
+/*
+ * Rows into their slots: row t of K and V (element e of head h at K[t*k_tok_stride + h*k_head_stride + e]) becomes row
+ * slots[t] % page_tokens of page slots[t] / page_tokens of the pools.  Rows t < min(rows, cu_new[batch]) are looked at (all
+ * `rows` if cu_new is NULL); a slot that is negative or behind the pool's last page leaves its row out.  K or V may be NULL
+ * (skipped).  Slots should differ: of two rows with one slot, either may be found there afterwards, in parts too.
+ * The rows must not overlap the pools.
+ */
+lightkv_status lightkv_page_write(const lightkv_pages *p, const int32_t *cu_new, const int32_t *slots, int64_t rows,
+                                  const void *K, int64_t k_tok_stride, int64_t k_head_stride,
+                                  const void *V, int64_t v_tok_stride, int64_t v_head_stride, void *stream);
+
+/* Bytes of workspace lightkv_page_attention needs (a bound over all lengths; 256-byte aligned memory). */
+lightkv_status lightkv_page_attention_workspace(const lightkv_pages *p, size_t *bytes);
+
+/*
+ * Attention of one new token per sequence: with q = Q[b, h], n = seq_lens[b] and k_t, v_t the rows of its K/V head,
+ *   out[b, h] = sum_{t < n} w_t v_t,  w_t = exp(q.k_t * scale - lse[h, b]),  lse[h, b] = log sum_{t < n} exp(q.k_t * scale).
+ * (The new token's own row counts if it was written and seq_lens says so.)  A sequence without tokens, or whose scores are all
+ * -inf, gets out = 0 and lse = -inf.  Tokens whose table entry is no page of the pool are left out.  NaN and infinities in
+ * rows behind the last token do not reach the result; those of rows that count do, as the formula says.
+ *   Q, out     element (b, h, e) at Q[b*q_tok_stride + h*q_head_stride + e], out alike; they must not overlap
+ *   softmax_scale   0 selects 1/sqrt(head_dim)
+ *   lse        [heads, batch] natural logarithm, may be NULL
+ *   max_seq_tokens  the caller's bound on seq_lens if it has one (0: max_pages * page_tokens).  It chooses how the work is
+ *              cut, nothing else: longer sequences are attended to in full
+ *   ws         two calls that share it must be ordered by their streams
+ * Scores, softmax and sums are fp32; weights enter the product with bf16 values as the sum of two bf16 numbers.  Where the
+ * length is split, the cut depends on the lengths of all sequences of the call, so the last bits of a sequence may differ in
+ * another batch; the same call gives the same bits.
+ */
+lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq_lens, int32_t max_seq_tokens,
+                                      const void *Q, int64_t q_tok_stride, int64_t q_head_stride, float softmax_scale,
+                                      void *out, int64_t o_tok_stride, int64_t o_head_stride, float *lse,
+                                      void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,6 +6,7 @@ There is no CPU fallback: importing `binding` without the built library raises.
 """
 from .binding import (  # noqa: F401
     LightKVError,
+    Pages,
     Problem,
     lib_path,
     lightkv_aggregate,
@@ -13,6 +14,11 @@ from .binding import (  # noqa: F401
     lightkv_build_windows,
     lightkv_build_windows_next,
     lightkv_compact,
+    lightkv_page_alloc,
+    lightkv_page_attention,
+    lightkv_page_attention_workspace,
+    lightkv_page_free,
+    lightkv_page_write,
     lightkv_score,
     lightkv_score_select,
     lightkv_select,
@@ -28,4 +34,4 @@ from .binding import (  # noqa: F401
     XI_GIVEN,
 )
 from .schedule import windows_per_sequence, max_window_cells  # noqa: F401
-from .pipeline import CompressionPipeline, EdgeTopKSchedule, from_device, to_device  # noqa: F401
+from .pipeline import CompressionPipeline, EdgeTopKSchedule, PagedCache, from_device, to_device  # noqa: F401

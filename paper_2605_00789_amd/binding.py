@@ -47,6 +47,17 @@ class _CStage(C.Structure):
     ]
 
 
+class _CPages(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int32), ("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("max_pages", C.c_int32),
+        ("table_stride", C.c_int64), ("table", C.c_void_p),
+        ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+        ("K", C.c_void_p), ("V", C.c_void_p),
+        ("k_page_stride", C.c_int64), ("k_tok_stride", C.c_int64), ("k_head_stride", C.c_int64),
+        ("v_page_stride", C.c_int64), ("v_tok_stride", C.c_int64), ("v_head_stride", C.c_int64),
+    ]
+
+
 def _load():
     path = lib_path()
     if not os.path.exists(path):
@@ -93,6 +104,17 @@ def _load():
     lib.lightkv_compress_schedule_ratio.restype = C.c_int
     lib.lightkv_compress_schedule_ratio.argtypes = [C.POINTER(_CStage), i32, C.POINTER(C.c_double), i32, i32, i32, vp, i64,
                                                     vp, i64, vp, i64, vp, vp, i64, i64, f32, vp, sz, vp, vp]
+    G = C.POINTER(_CPages)
+    lib.lightkv_page_alloc.restype = C.c_int
+    lib.lightkv_page_alloc.argtypes = [G, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp]
+    lib.lightkv_page_free.restype = C.c_int
+    lib.lightkv_page_free.argtypes = [G, vp, vp, vp, vp, vp, vp, vp]
+    lib.lightkv_page_write.restype = C.c_int
+    lib.lightkv_page_write.argtypes = [G, vp, vp, i64, vp, i64, i64, vp, i64, i64, vp]
+    lib.lightkv_page_attention_workspace.restype = C.c_int
+    lib.lightkv_page_attention_workspace.argtypes = [G, C.POINTER(sz)]
+    lib.lightkv_page_attention.restype = C.c_int
+    lib.lightkv_page_attention.argtypes = [G, vp, i32, vp, i64, i64, f32, vp, i64, i64, vp, vp, sz, vp]
     return lib
 
 
@@ -101,7 +123,8 @@ _lib = _load()
 EXPORTS = ("lightkv_status_string", "lightkv_version", "lightkv_workspace_size", "lightkv_build_windows", "lightkv_compress_schedule",
            "lightkv_compress_schedule_ratio",
            "lightkv_build_windows_next", "lightkv_windows_per_sequence", "lightkv_max_window_cells", "lightkv_window_counts",
-           "lightkv_score", "lightkv_score_select", "lightkv_select", "lightkv_select_static", "lightkv_aggregate", "lightkv_compact", "lightkv_aggregate_compact")
+           "lightkv_score", "lightkv_score_select", "lightkv_select", "lightkv_select_static", "lightkv_aggregate", "lightkv_compact", "lightkv_aggregate_compact",
+           "lightkv_page_alloc", "lightkv_page_free", "lightkv_page_write", "lightkv_page_attention_workspace", "lightkv_page_attention")
 
 
 def _dptr(t: Optional[torch.Tensor]):
@@ -354,3 +377,128 @@ def lightkv_compress_schedule_ratio(stages: StageArray, rho, tiles, grid_h, grid
                                                 ws.numel() * ws.element_size(), h_out.ctypes.data_as(C.c_void_p),
                                                 _stream(stream)), "lightkv_compress_schedule_ratio")
     return h_out
+
+
+# ---- paged cache ------------------------------------------------------------------------------------------------------
+PAGED_MAX_BATCH = 4096   # LIGHTKV_PAGED_MAX_BATCH
+_PAGE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+class Pages:
+    """Python mirror of `lightkv_pages`; keeps the tensors it points to alive.
+    table: int32 [batch, max_pages].  K, V: the pools, [n_pages, page_tokens, kv_heads, head_dim] views of any strides (pages
+    stored head-major are handed in as pool.transpose(1, 2)); heads: query heads.  Without K and V (tables only): n_pages
+    and page_tokens."""
+
+    def __init__(self, table, *, K=None, V=None, heads=0, n_pages=0, page_tokens=0):
+        if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table: int32 [batch, max_pages] with contiguous rows")
+        self.refs = (table, K, V)
+        self.device = table.device
+        c = self.c = _CPages()
+        c.batch, c.max_pages = int(table.shape[0]), int(table.shape[1])
+        c.table, c.table_stride = _dptr(table), (int(table.stride(0)) if c.batch > 1 else max(int(table.stride(0)), c.max_pages))
+        self.dtype = None
+        for name, t in (("k", K), ("v", V)):
+            if t is None:
+                continue
+            if t.dim() != 4 or t.dtype not in _PAGE_DTYPES or t.device != self.device or t.stride(3) != 1:
+                raise ValueError("pools: float32 or bfloat16 [n_pages, page_tokens, kv_heads, head_dim] on the table's device")
+            if self.dtype is not None and (t.dtype != self.dtype or tuple(t.shape) != self.shape):
+                raise ValueError("K and V pools differ in type or shape")
+            self.dtype, self.shape = t.dtype, tuple(t.shape)
+            setattr(c, name.upper(), _dptr(t))
+            for what, axis in (("page", 0), ("tok", 1), ("head", 2)):
+                setattr(c, "%s_%s_stride" % (name, what), int(t.stride(axis)))
+        if self.dtype is not None:
+            n, p, h, d = self.shape
+            if n_pages not in (0, n) or page_tokens not in (0, p):
+                raise ValueError("n_pages or page_tokens differ from the pools'")
+            c.n_pages, c.page_tokens, c.kv_heads, c.head_dim, c.dtype = n, p, h, d, _PAGE_DTYPES[self.dtype]
+            c.heads = int(heads) if heads else h
+        else:
+            c.n_pages, c.page_tokens = int(n_pages), int(page_tokens)
+        self._ref = C.byref(c)
+
+    def _ints(self, t, n, what):
+        """An int32 array of at least n entries on the cache's device."""
+        if t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous() or t.numel() < n:
+            raise ValueError("%s: contiguous int32 of at least %d entries on the table's device" % (what, n))
+        return t.data_ptr()
+
+    def _rows(self, t, heads, n, what):
+        """Rows [n or more, heads, head_dim] (or [.., heads * head_dim]): pointer and strides."""
+        d = self.c.head_dim
+        if t.dtype != self.dtype or t.device != self.device:
+            raise ValueError("%s: %s on the table's device" % (what, self.dtype))
+        if t.dim() == 3 and t.shape[1] == heads and t.shape[2] == d and t.stride(2) == 1 and t.shape[0] >= n:
+            return t.data_ptr(), t.stride(0), t.stride(1)
+        if t.dim() == 2 and t.shape[1] == heads * d and t.stride(1) == 1 and t.shape[0] >= n:
+            return t.data_ptr(), t.stride(0), d
+        raise ValueError("%s: [%d or more, %d, %d] with contiguous elements" % (what, n, heads, d))
+
+    def _call(self, fn, where, args, stream):
+        """The call on its stream: that of the cache's device, with this device current."""
+        if torch.cuda.current_device() == self.device.index:
+            s = torch.cuda.current_stream() if stream is None else stream
+            st = fn(self._ref, *args, s.cuda_stream)
+        else:
+            with torch.cuda.device(self.device):
+                s = torch.cuda.current_stream() if stream is None else stream
+                st = fn(self._ref, *args, s.cuda_stream)
+        if st != 0:
+            raise LightKVError(st, where)
+
+
+def lightkv_page_alloc(p: Pages, cu_new, seq_lens, free_pages, free_count, seq_lens_out, free_count_out, slots, *,
+                       status=None, stream=None):
+    """Pages and slots for cu_new[b + 1] - cu_new[b] more tokens of every sequence; seq_lens_out and free_count_out may be
+    seq_lens and free_count themselves."""
+    n, ints = p.c.batch, p._ints
+    args = (ints(cu_new, n + 1, "cu_new"), ints(seq_lens, n, "seq_lens"), ints(free_pages, p.c.n_pages, "free_pages"),
+            ints(free_count, 1, "free_count"), ints(seq_lens_out, n, "seq_lens_out"),
+            ints(free_count_out, 1, "free_count_out"), ints(slots, 0, "slots"), slots.numel(),
+            None if status is None else ints(status, n, "status"))
+    p._call(_lib.lightkv_page_alloc, "lightkv_page_alloc", args, stream)
+
+
+def lightkv_page_free(p: Pages, done, seq_lens, free_pages, free_count, seq_lens_out, free_count_out, *, stream=None):
+    """Pages of every sequence with done[b] != 0 back onto the stack."""
+    n, ints = p.c.batch, p._ints
+    args = (ints(done, n, "done"), ints(seq_lens, n, "seq_lens"), ints(free_pages, p.c.n_pages, "free_pages"),
+            ints(free_count, 1, "free_count"), ints(seq_lens_out, n, "seq_lens_out"),
+            ints(free_count_out, 1, "free_count_out"))
+    p._call(_lib.lightkv_page_free, "lightkv_page_free", args, stream)
+
+
+def lightkv_page_write(p: Pages, slots, K, V, *, cu_new=None, stream=None):
+    """Rows K, V [rows, kv_heads, head_dim] (or [rows, kv_heads * head_dim]) into their slots; with cu_new only the first
+    cu_new[batch] of them.  K or V may be None."""
+    rows = min(t.shape[0] for t in (K, V, slots) if t is not None)
+    if rows == 0:
+        return
+    h = p.c.kv_heads
+    k = (None, 0, 0) if K is None else p._rows(K, h, rows, "K")
+    v = (None, 0, 0) if V is None else p._rows(V, h, rows, "V")
+    args = (None if cu_new is None else p._ints(cu_new, p.c.batch + 1, "cu_new"), p._ints(slots, rows, "slots"), rows, *k, *v)
+    p._call(_lib.lightkv_page_write, "lightkv_page_write", args, stream)
+
+
+def lightkv_page_attention_workspace(p: Pages) -> int:
+    out = C.c_size_t(0)
+    _check(_lib.lightkv_page_attention_workspace(p._ref, C.byref(out)), "lightkv_page_attention_workspace")
+    return int(out.value)
+
+
+def lightkv_page_attention(p: Pages, seq_lens, Q, out, ws, *, lse=None, softmax_scale=0.0, max_seq_tokens=0, stream=None):
+    """Attention of one new token per sequence: Q, out [batch, heads, head_dim] (or [batch, heads * head_dim]); lse: optional
+    fp32 [heads, batch]; ws: uint8 of lightkv_page_attention_workspace(p) bytes."""
+    c = p.c
+    if lse is not None and (lse.dtype != torch.float32 or lse.device != p.device or not lse.is_contiguous() or lse.numel() < c.heads * c.batch):
+        raise ValueError("lse: contiguous float32 [heads, batch] on the table's device")
+    if ws.device != p.device:
+        raise ValueError("ws on the table's device")
+    args = (p._ints(seq_lens, c.batch, "seq_lens"), int(max_seq_tokens), *p._rows(Q, c.heads, c.batch, "Q"), float(softmax_scale),
+            *p._rows(out, c.heads, c.batch, "out"), None if lse is None else lse.data_ptr(), ws.data_ptr(),
+            ws.numel() * ws.element_size())
+    p._call(_lib.lightkv_page_attention, "lightkv_page_attention", args, stream)

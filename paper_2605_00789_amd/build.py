@@ -11,14 +11,15 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "liblightkv.so")
 PROBE_LIB_PATH = os.path.join(HERE, "liblightkv_probe.so")   # measurement kernels for bench.py --pass ceilings, nothing of the method
-SOURCES = ["lk_api.hip", "lk_windows.hip", "lk_score_fd.hip", "lk_score_fd_big.hip", "lk_fd_dump.hip", "lk_score_xi.hip", "lk_xi_seq.hip", "lk_select.hip", "lk_select_edges.hip", "lk_select_pair.hip", "lk_rows.hip", "lk_fused.hip", "lk_schedule.hip"]
+SOURCES = ["lk_api.hip", "lk_windows.hip", "lk_score_fd.hip", "lk_score_fd_big.hip", "lk_fd_dump.hip", "lk_score_xi.hip", "lk_xi_seq.hip", "lk_select.hip", "lk_select_edges.hip", "lk_select_pair.hip", "lk_rows.hip", "lk_fused.hip", "lk_schedule.hip",
+           "lk_pages.hip", "lk_page_attn.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed-fp32 instruction forms are kept out of the generated code on purpose
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 # matrix-core results that vector instructions go on with at once: left alone the compiler puts them into accumulation
 # registers and copies every one of them out (16 copies per 32 x 32 tile)
 FILE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-              for src in ("lk_score_xi.hip", "lk_fused.hip")}
+              for src in ("lk_score_xi.hip", "lk_fused.hip", "lk_page_attn.hip")}
 
 
 def _hipcc() -> str:

@@ -1,0 +1,521 @@
+// Attention of one new token per sequence over a paged K/V cache (lightkv_page_attention).
+//
+//   s_t = q.k_t * scale,   m = max s_t,   l = sum exp(s_t - m),   out = sum exp(s_t - m) v_t / l,   lse = m + log l
+//
+// One pass over K and V with the running maximum and sum of a softmax; parts of a sequence (waves, workgroups) keep (m, l, o)
+// of their own and are joined as l = sum l_i exp(m_i - m), o alike.  4 flops for each element that is read: the bytes of K and
+// V bound it, at any number of query heads a K/V head serves.  So the matrix instructions are there to keep the vector units
+// out of the way: up to 16 query heads of a K/V head are the columns of one 16 x 16 block, and fewer cost the same.
+//
+// Nothing of K or V passes through LDS.  A tile is 32 tokens (16 for fp32) of one K/V head, and a lane (m = lane % 16,
+// g = lane / 16) loads
+//   K: token 16 h + m, 16-byte chunks g, g + 4, ..  = rows of the first product's A operand (S^T = K Q^T),
+//   V: tokens 16 h + 4 g + i, elements m * head_dim / 16 ..  (16 lanes read a whole row).
+// S^T leaves lane (m, g) with the scores of query m against tokens 16 h + 4 g + i: as they stand the B operand of
+// out^T = V^T P^T, since a product does not care how the tokens it sums over are numbered as long as both sides agree.  V's
+// operand wants one element of eight tokens in a lane, where a lane holds several elements of each of its eight tokens: a
+// transposition inside the lane, one byte permutation per register (fp32: none).  Output rows come out permuted, element
+// m * head_dim / 16 + t for row m of block t, which the store undoes.
+#include "lk_common.h"
+#include "lk_pages.h"
+
+namespace lk {
+
+constexpr int PA_MAX_Q = 16;     // query heads per block
+constexpr float PA_LOG2E = 1.4426950408889634f, PA_LN2 = 0.6931471805599453f;
+
+struct PageAttnArgs {
+  const char *K, *V, *Q;
+  char *out;
+  float *lse, *stats, *part;      // records of partial results: (m, l) and unscaled sums
+  const int32_t *table, *seq_lens;
+  int64_t table_stride;
+  int64_t k_page, k_tok, k_head, v_page, v_tok, v_head, q_tok, q_head, o_tok, o_head;   // bytes
+  int batch, kv_heads, group, q_blocks;   // query heads per K/V head, blocks of at most 16 of them
+  int n_pages, lg, room;          // room: tokens a table row can hold
+  int n_wgs, min_tiles;           // split launches: workgroups, and the fewest tiles one takes
+  float scale2;                   // softmax scale * log2(e)
+};
+
+template <typename T, int HD> struct PaGeo {
+  static constexpr int EB = Elem<T>::BYTES;
+  static constexpr int TILE = EB == 2 ? 32 : 16;   // tokens
+  static constexpr int NH = TILE / 16;             // 16-token halves
+  static constexpr int KL = HD * EB / 64;          // 16-byte loads per lane and K row
+  static constexpr int NK = TILE / 4;              // V rows per lane
+  static constexpr int VT = HD / 16;               // elements per lane and V row, = output blocks
+  static constexpr int VW = VT * EB / 4;           // ... in words
+};
+
+template <typename T, int HD> struct PaTile {
+  using G = PaGeo<T, HD>;
+  uint4 k[G::NH][G::KL];
+  uint32_t v[G::NK][G::VW];
+  uint32_t live;                                   // bit t: token t of the tile counts
+};
+
+template <int W> __device__ __forceinline__ void pa_load_words(uint32_t (&d)[W], const char *p) {
+  if constexpr (W % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) {
+      const uint4 v = ld16(p + i * 4);
+      d[i] = v.x; d[i + 1] = v.y; d[i + 2] = v.z; d[i + 3] = v.w;
+    }
+  } else if constexpr (W == 2) {
+    const uint2 v = *reinterpret_cast<const uint2 *>(p);
+    d[0] = v.x; d[1] = v.y;
+  } else {
+    d[0] = *reinterpret_cast<const uint32_t *>(p);
+  }
+}
+
+// One wave's share of a segment: (m, l, o) of up to 16 queries.  m belongs to query lane % 16 in all four lane groups, l holds
+// the lane's own tokens until it is summed at the end.
+template <typename T, int HD> struct PaState {
+  using G = PaGeo<T, HD>;
+  float m, l;
+  f32x4 o[G::VT];
+};
+
+template <typename T, int HD>
+__device__ __forceinline__ void pa_accumulate(PaState<T, HD> &st, PaTile<T, HD> &tile, const uint4 (&q)[PaGeo<T, HD>::KL], float scale2, int g) {
+  using G = PaGeo<T, HD>;
+  float s[G::NH][4];
+#pragma unroll
+  for (int h = 0; h < G::NH; ++h) {
+    f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < G::KL; ++i) {
+      if constexpr (G::EB == 2) {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, tile.k[h][i]), __builtin_bit_cast(bf16x8, q[i]), c, 0, 0, 0);
+      } else {
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tile.k[h][i].x), __uint_as_float(q[i].x), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tile.k[h][i].y), __uint_as_float(q[i].y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tile.k[h][i].z), __uint_as_float(q[i].z), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tile.k[h][i].w), __uint_as_float(q[i].w), c, 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[h][i] = c[i] * scale2;
+  }
+  constexpr uint32_t ALL = G::TILE == 32 ? 0xffffffffu : 0xffffu;
+  if (tile.live != ALL) {   // (the same in all lanes)
+#pragma unroll
+    for (int h = 0; h < G::NH; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool dead = !((tile.live >> (h * 16 + g * 4 + i)) & 1u);
+        if (dead) s[h][i] = -INFINITY;
+        // a weight of zero does not silence a NaN or an infinity: the row itself becomes zero
+#pragma unroll
+        for (int w = 0; w < G::VW; ++w) tile.v[h * 4 + i][w] = dead ? 0u : tile.v[h * 4 + i][w];
+      }
+  }
+  float mx = s[0][0];
+#pragma unroll
+  for (int h = 0; h < G::NH; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[h][i]);
+  // the maximum moves about log(tiles) times: only then do lanes compare and sums get rescaled
+  if (__ballot(mx > st.m)) {
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m = fmaxf(st.m, mx);
+    const float a = m == st.m ? 1.f : __builtin_amdgcn_exp2f(st.m - m);
+    st.m = m;
+    st.l *= a;
+#pragma unroll
+    for (int t = 0; t < G::VT; ++t) st.o[t] *= a;
+  }
+  const float ref = st.m == -INFINITY ? 0.f : st.m;
+  float p[G::NH][4];
+#pragma unroll
+  for (int h = 0; h < G::NH; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      p[h][i] = __builtin_amdgcn_exp2f(s[h][i] - ref);
+      st.l += p[h][i];
+    }
+  if constexpr (G::EB == 2) {
+    // weights as hi + lo, two bf16 numbers: what is cut off lies 2^-15 below the weight, so the product is as good as an
+    // fp32 one; the second matrix instruction is free beside the loads (one bf16 number per weight: 2^-8)
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t a = __float_as_uint(p[j >> 1][(j & 1) * 2]), b = __float_as_uint(p[j >> 1][(j & 1) * 2 + 1]);
+      hi[j] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      const float ra = __uint_as_float(a) - __uint_as_float(a & 0xffff0000u), rb = __uint_as_float(b) - __uint_as_float(b & 0xffff0000u);
+      lo[j] = __builtin_amdgcn_perm(__float_as_uint(rb), __float_as_uint(ra), 0x07060302u);
+    }
+    const bf16x8 ph = __builtin_bit_cast(bf16x8, uint4{hi[0], hi[1], hi[2], hi[3]}), pl = __builtin_bit_cast(bf16x8, uint4{lo[0], lo[1], lo[2], lo[3]});
+#pragma unroll
+    for (int t = 0; t < G::VT; ++t) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = __builtin_amdgcn_perm(tile.v[2 * j + 1][t >> 1], tile.v[2 * j][t >> 1], (t & 1) ? 0x07060302u : 0x05040100u);
+      const bf16x8 vt = __builtin_bit_cast(bf16x8, uint4{w[0], w[1], w[2], w[3]});
+      st.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, ph, st.o[t], 0, 0, 0);
+      st.o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pl, st.o[t], 0, 0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < G::VT; ++t)
+        st.o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tile.v[i][t]), p[0][i], st.o[t], 0, 0, 0);
+  }
+}
+
+// Tiles t0 + wave, t0 + wave + WAVES, .. < t1 of sequence b, K/V head h, query heads h0 .. h0 + gq - 1.  While a tile is
+// worked on the next one of the wave is on its way, and the page numbers of the one behind that.
+template <typename T, int HD, int WAVES>
+__device__ __forceinline__ void pa_run(const PageAttnArgs &a, int b, int len, int h, int h0, int gq, int t0, int t1, PaState<T, HD> &st) {
+  using G = PaGeo<T, HD>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
+  st.m = -INFINITY;
+  st.l = 0.f;
+#pragma unroll
+  for (int t = 0; t < G::VT; ++t) st.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int t = t0 + wave;
+  if (t >= t1) return;
+  const int32_t *row = a.table + (int64_t)b * a.table_stride;
+  const int in_page = (1 << a.lg) - 1;
+  // page of token lane % TILE of a tile; -1: does not count
+  auto pages_of = [&](int tile) {
+    const int key = tile * G::TILE + (lane & (G::TILE - 1));
+    int pg = -1;
+    if (key < len) pg = row[key >> a.lg];
+    return (unsigned)pg < (unsigned)a.n_pages ? pg : -1;
+  };
+  const char *kh = a.K + (int64_t)h * a.k_head + g * 16, *vh = a.V + (int64_t)h * a.v_head + m * (G::VW * 4);
+  // rows that do not count are read from page 0 (any row of the pool will do) and masked
+  auto load = [&](PaTile<T, HD> &d, int tile, int pg) {
+    d.live = (uint32_t)__ballot(pg >= 0) & (G::TILE == 32 ? 0xffffffffu : 0xffffu);
+    const int key0 = tile * G::TILE, safe = pg < 0 ? 0 : pg;
+#pragma unroll
+    for (int hh = 0; hh < G::NH; ++hh) {
+      const int page = __shfl(safe, hh * 16 + m, 64);
+      const char *p = kh + (int64_t)page * a.k_page + (int64_t)((key0 + hh * 16 + m) & in_page) * a.k_tok;
+#pragma unroll
+      for (int i = 0; i < G::KL; ++i) d.k[hh][i] = ld16(p + i * 64);
+    }
+#pragma unroll
+    for (int hh = 0; hh < G::NH; ++hh) {
+      const int page = __shfl(safe, hh * 16 + g * 4, 64);   // (four tokens from a multiple of four share a page)
+      const char *p = vh + (int64_t)page * a.v_page + (int64_t)((key0 + hh * 16 + g * 4) & in_page) * a.v_tok;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pa_load_words<G::VW>(d.v[hh * 4 + i], p + i * a.v_tok);
+    }
+  };
+  uint4 q[G::KL];
+#pragma unroll
+  for (int i = 0; i < G::KL; ++i) q[i] = uint4{0u, 0u, 0u, 0u};
+  if (m < gq) {
+    const char *p = a.Q + (int64_t)b * a.q_tok + (int64_t)(h0 + m) * a.q_head + g * 16;
+#pragma unroll
+    for (int i = 0; i < G::KL; ++i) q[i] = ld16(p + i * 64);
+  }
+  PaTile<T, HD> x, y;
+  int next = pages_of(t);
+  load(x, t, next);
+  next = pages_of(t + WAVES < t1 ? t + WAVES : t);
+  for (;;) {
+    if (t + WAVES < t1) {
+      load(y, t + WAVES, next);
+      next = pages_of(t + 2 * WAVES < t1 ? t + 2 * WAVES : t);
+    }
+    pa_accumulate<T, HD>(st, x, q, a.scale2, g);
+    t += WAVES;
+    if (t >= t1) break;
+    if (t + WAVES < t1) {
+      load(x, t + WAVES, next);
+      next = pages_of(t + 2 * WAVES < t1 ? t + 2 * WAVES : t);
+    }
+    pa_accumulate<T, HD>(st, y, q, a.scale2, g);
+    t += WAVES;
+    if (t >= t1) break;
+  }
+}
+
+template <typename T> __device__ __forceinline__ void pa_store(char *p, float v);
+template <> __device__ __forceinline__ void pa_store<float>(char *p, float v) { *reinterpret_cast<float *>(p) = v; }
+template <> __device__ __forceinline__ void pa_store<bf16_t>(char *p, float v) { *reinterpret_cast<uint16_t *>(p) = (uint16_t)f32_to_bf16_rne(v); }
+
+// Result of one query element: o / l, zero where nothing counted (l = 0; a NaN goes through).
+template <typename T>
+__device__ __forceinline__ void pa_finish(const PageAttnArgs &a, int b, int head, int d, float m, float l, float o) {
+  pa_store<T>(a.out + (int64_t)b * a.o_tok + (int64_t)head * a.o_head + d * Elem<T>::BYTES, l == 0.f ? 0.f : o / l);
+  if (d == 0 && a.lse) a.lse[(int64_t)head * a.batch + b] = l == 0.f ? -INFINITY : (m + log2f(l)) * PA_LN2;
+}
+
+constexpr int PA_PAD = 4;   // words between the rows of two queries
+template <int HD> __host__ __device__ constexpr size_t pa_join_floats(int waves, int gq) { return (size_t)waves * gq * (HD + PA_PAD + 2); }
+
+// The waves' parts joined in LDS; record < 0: the result, otherwise a record of partial sums.
+template <typename T, int HD, int WAVES>
+__device__ __forceinline__ void pa_join(const PageAttnArgs &a, float *lds, PaState<T, HD> &st, int b, int h0, int gq, int record) {
+  using G = PaGeo<T, HD>;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  float *so = lds, *ss = lds + (size_t)WAVES * gq * (HD + PA_PAD);
+  float l = st.l;
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (m < gq) {
+    float *to = so + (size_t)(wave * gq + m) * (HD + PA_PAD);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < G::VT; ++t) to[(g * 4 + i) * G::VT + t] = st.o[t][i];
+    if (g == 0) { ss[(wave * gq + m) * 2] = st.m; ss[(wave * gq + m) * 2 + 1] = l; }
+  }
+  __syncthreads();
+  const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q;   // of a record
+  for (int i = threadIdx.x; i < gq * HD; i += WAVES * 64) {
+    const int n = i / HD, d = i % HD;
+    float top = -INFINITY, sum = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ss[(w * gq + n) * 2]);
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float mw = ss[(w * gq + n) * 2], f = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - ref);
+      sum += f * ss[(w * gq + n) * 2 + 1];
+      o += f * so[(size_t)(w * gq + n) * (HD + PA_PAD) + d];
+    }
+    if (record < 0) {
+      pa_finish<T>(a, b, h0 + n, d, top, sum, o);
+    } else {
+      const int64_t r = (int64_t)record * rows + n;
+      a.part[r * HD + d] = o;
+      if (d == 0) { a.stats[r * 2] = top; a.stats[r * 2 + 1] = sum; }
+    }
+  }
+}
+
+__device__ __forceinline__ int pa_len(const PageAttnArgs &a, int b) {
+  const int n = a.seq_lens[b];
+  return n < 0 ? 0 : (n < a.room ? n : a.room);
+}
+
+// One workgroup per (sequence, block of query heads): the whole length, no second launch.
+template <typename T, int HD, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void page_attn_whole_kernel(PageAttnArgs a) {
+  fetch_args<PageAttnArgs>();
+  extern __shared__ float pa_lds[];
+  const int segs = a.kv_heads * a.q_blocks, b = blockIdx.x / segs, seg = blockIdx.x - b * segs;
+  const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
+  const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
+  const int len = pa_len(a, b);
+  PaState<T, HD> st;
+  pa_run<T, HD, WAVES>(a, b, len, h, h0, gq, 0, (len + PaGeo<T, HD>::TILE - 1) / PaGeo<T, HD>::TILE, st);
+  pa_join<T, HD, WAVES>(a, pa_lds, st, b, h0, gq, -1);
+}
+
+// Split launches.  All tiles of the call, sequence by sequence and in it head by head, are one line that is cut into pieces of
+// equal length, a workgroup each: the cut goes by what there is to do, whatever the lengths are, and needs nothing from the host.
+// A piece covers the end of a segment, whole segments, and the beginning of another: whole ones are finished at once, the two
+// parts become records 2 w and 2 w + 1, which the second kernel joins.
+struct PaCut { int total; int64_t tiles, piece; };
+
+// before[b] = tiles of one head in the sequences before b; the whole workgroup.
+__device__ __forceinline__ PaCut pa_cut(const PageAttnArgs &a, int tile, int segs, int *before, int *scratch) {
+  const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (a.batch + threads - 1) / threads, b0 = tid * per, b1 = b0 + per < a.batch ? b0 + per : a.batch;
+  int mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    before[b] = (pa_len(a, b) + tile - 1) / tile;
+    mine += before[b];
+  }
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 63) scratch[wave] = incl;
+  __syncthreads();
+  int at = incl - mine, total = 0;
+  for (int w = 0; w < threads / 64; ++w) {
+    if (w < wave) at += scratch[w];
+    total += scratch[w];
+  }
+  for (int b = b0; b < b1; ++b) {
+    const int n = before[b];
+    before[b] = at;
+    at += n;
+  }
+  if (tid == 0) before[a.batch] = total;
+  __syncthreads();
+  PaCut c;
+  c.total = total;
+  c.tiles = (int64_t)total * segs;
+  c.piece = (c.tiles + a.n_wgs - 1) / a.n_wgs;
+  c.piece = c.piece < a.min_tiles ? a.min_tiles : c.piece;
+  return c;
+}
+
+template <typename T, int HD, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void page_attn_split_kernel(PageAttnArgs a) {
+  fetch_args<PageAttnArgs>();
+  extern __shared__ float pa_lds[];
+  __shared__ int scratch[WAVES];
+  const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, segs = a.kv_heads * a.q_blocks;
+  int *before = reinterpret_cast<int *>(pa_lds + pa_join_floats<HD>(WAVES, rows));
+  const PaCut c = pa_cut(a, PaGeo<T, HD>::TILE, segs, before, scratch);
+  int64_t at = (int64_t)blockIdx.x * c.piece;
+  const int64_t end = at + c.piece < c.tiles ? at + c.piece : c.tiles;
+  if (at >= end) return;
+  int lo = 0, hi = a.batch;    // last sequence that begins at or before `at`
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if ((int64_t)before[mid] * segs <= at) lo = mid;
+    else hi = mid;
+  }
+  int b = lo;
+  while (at < end) {
+    while (before[b + 1] == before[b] || (int64_t)before[b + 1] * segs <= at) ++b;   // (ends: at < tiles)
+    const int nt = before[b + 1] - before[b];
+    const int64_t local = at - (int64_t)before[b] * segs;
+    const int seg = (int)(local / nt), t0 = (int)(local - (int64_t)seg * nt);
+    const int t1 = end - at < nt - t0 ? t0 + (int)(end - at) : nt;
+    const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
+    const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
+    PaState<T, HD> st;
+    pa_run<T, HD, WAVES>(a, b, pa_len(a, b), h, h0, gq, t0, t1, st);
+    const int record = t0 == 0 && t1 == nt ? -1 : 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
+    pa_join<T, HD, WAVES>(a, pa_lds, st, b, h0, gq, record);
+    at += t1 - t0;
+    __syncthreads();
+  }
+}
+
+constexpr int PA_JOIN_THREADS = 256;
+
+// Joins the records of one segment, and writes what sequences without tokens get.
+template <typename T, int HD>
+__global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAttnArgs a) {
+  fetch_args<PageAttnArgs>();
+  extern __shared__ float pa_lds[];
+  __shared__ int scratch[PA_JOIN_THREADS / 64];
+  const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, segs = a.kv_heads * a.q_blocks;
+  int *before = reinterpret_cast<int *>(pa_lds);
+  const PaCut c = pa_cut(a, PaGeo<T, HD>::TILE, segs, before, scratch);
+  const int b = blockIdx.x / segs, seg = blockIdx.x - b * segs, nt = before[b + 1] - before[b];
+  const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
+  const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
+  const int64_t first = (int64_t)before[b] * segs + (int64_t)seg * nt;
+  const int w0 = nt ? (int)(first / c.piece) : 0, w1 = nt ? (int)((first + nt - 1) / c.piece) : -1;
+  if (nt && w0 == w1) return;    // one workgroup had it all
+  for (int i = threadIdx.x; i < gq * HD; i += PA_JOIN_THREADS) {
+    const int n = i / HD, d = i % HD;
+    float top = -INFINITY, sum = 0.f, o = 0.f;
+    for (int w = w0; w <= w1; ++w) top = fmaxf(top, a.stats[((int64_t)(2 * w + (w == w0 ? 1 : 0)) * rows + n) * 2]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    for (int w = w0; w <= w1; ++w) {
+      const int64_t r = (int64_t)(2 * w + (w == w0 ? 1 : 0)) * rows + n;
+      const float mw = a.stats[r * 2], f = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - ref);
+      sum += f * a.stats[r * 2 + 1];
+      o += f * a.part[r * HD + d];
+    }
+    pa_finish<T>(a, b, h0 + n, d, top, sum, o);
+  }
+}
+
+constexpr int PA_WGS = 512;          // workgroups of a split launch: two of four waves fit a CU
+constexpr int PA_WHOLE_TOKENS = 1024;
+
+inline int pa_rows(const lightkv_pages *p) { const int g = p->heads / p->kv_heads; return g < PA_MAX_Q ? g : PA_MAX_Q; }
+inline size_t pa_stat_bytes(const lightkv_pages *p) { return ((size_t)2 * PA_WGS * pa_rows(p) * 2 * sizeof(float) + 255) / 256 * 256; }
+inline size_t pa_part_bytes(const lightkv_pages *p) { return (size_t)2 * PA_WGS * pa_rows(p) * p->head_dim * sizeof(float); }
+
+template <typename T, int HD>
+static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t stream) {
+  const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q;
+  const unsigned segs = (unsigned)a.batch * (unsigned)(a.kv_heads * a.q_blocks);
+  if (whole) {
+    if (rows <= 8) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), pa_join_floats<HD>(8, rows) * sizeof(float), stream, a);
+    else hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 4>), dim3(segs), dim3(256), pa_join_floats<HD>(4, rows) * sizeof(float), stream, a);
+    return hipGetLastError();
+  }
+  const size_t cut = ((size_t)a.batch + 1) * sizeof(int);
+  hipLaunchKernelGGL((page_attn_split_kernel<T, HD, 4>), dim3(a.n_wgs), dim3(256), pa_join_floats<HD>(4, rows) * sizeof(float) + cut, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((page_attn_join_kernel<T, HD>), dim3(segs), dim3(PA_JOIN_THREADS), cut, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace lk
+
+using namespace lk;
+
+namespace {
+lightkv_status check_page_attention(const lightkv_pages *p) {
+  const lightkv_status st = check_page_pools(p, true);
+  if (st != LIGHTKV_OK) return st;
+  // tiles are counted in 32 bits, workgroups and their threads too
+  if ((int64_t)p->batch * (((int64_t)p->max_pages * p->page_tokens + 15) / 16) >= (1ll << 31)) return LIGHTKV_ERR_UNSUPPORTED;
+  if ((int64_t)p->batch * p->heads >= (1ll << 22)) return LIGHTKV_ERR_UNSUPPORTED;
+  return LIGHTKV_OK;
+}
+}  // namespace
+
+extern "C" {
+
+lightkv_status lightkv_page_attention_workspace(const lightkv_pages *p, size_t *bytes) {
+  if (!bytes) return LIGHTKV_ERR_NULL;
+  const lightkv_status st = check_page_attention(p);
+  if (st == LIGHTKV_OK) *bytes = pa_stat_bytes(p) + pa_part_bytes(p);
+  return st;
+}
+
+lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq_lens, int32_t max_seq_tokens,
+                                      const void *Q, int64_t q_tok_stride, int64_t q_head_stride, float softmax_scale,
+                                      void *out, int64_t o_tok_stride, int64_t o_head_stride, float *lse,
+                                      void *ws, size_t ws_bytes, void *stream) {
+  lightkv_status st = check_page_attention(p);
+  if (st != LIGHTKV_OK) return st;
+  if (!seq_lens || !Q || !out) return LIGHTKV_ERR_NULL;
+  if (!(softmax_scale >= 0.f && softmax_scale <= 3.4e38f) || max_seq_tokens < 0) return LIGHTKV_ERR_SHAPE;   // (NaN too)
+  if (!aligned_to(seq_lens, 4) || !aligned_to(lse, 4)) return LIGHTKV_ERR_UNSUPPORTED;
+  const int eb = page_elem_bytes(p);
+  st = check_strided(Q, eb, q_tok_stride, p->batch, q_head_stride, p->heads);
+  if (st == LIGHTKV_OK) st = check_strided(out, eb, o_tok_stride, p->batch, o_head_stride, p->heads);
+  if (st != LIGHTKV_OK) return st;
+  const uint64_t out_bytes = strided_bytes(eb, o_tok_stride, p->batch, o_head_stride, p->heads, p->head_dim);
+  const uint64_t lse_bytes = lse ? (uint64_t)p->heads * p->batch * 4 : 0, len_bytes = (uint64_t)p->batch * 4;
+  if (overlap(Q, strided_bytes(eb, q_tok_stride, p->batch, q_head_stride, p->heads, p->head_dim), out, out_bytes)) return LIGHTKV_ERR_SHAPE;
+  if (overlap(lse, lse_bytes, out, out_bytes) || overlap(seq_lens, len_bytes, out, out_bytes) || overlap(seq_lens, len_bytes, lse, lse_bytes)) return LIGHTKV_ERR_SHAPE;
+  const uint64_t k_bytes = pool_bytes(p, p->k_page_stride, p->k_tok_stride, p->k_head_stride), v_bytes = pool_bytes(p, p->v_page_stride, p->v_tok_stride, p->v_head_stride);
+  if (overlap(p->K, k_bytes, out, out_bytes) || overlap(p->V, v_bytes, out, out_bytes) || overlap(ws, ws_bytes, out, out_bytes)) return LIGHTKV_ERR_SHAPE;
+  // rows of the output must not share elements
+  if (p->heads > 1 && o_head_stride < p->head_dim) return LIGHTKV_ERR_SHAPE;
+  if (p->batch > 1 && o_tok_stride < p->head_dim) return LIGHTKV_ERR_SHAPE;
+  const size_t stat = pa_stat_bytes(p);
+  if (!ws || !aligned_to(ws, 256) || ws_bytes < stat + pa_part_bytes(p)) return LIGHTKV_ERR_WORKSPACE;
+  PageAttnArgs a{};
+  a.K = static_cast<const char *>(p->K); a.V = static_cast<const char *>(p->V);
+  a.Q = static_cast<const char *>(Q); a.out = static_cast<char *>(out); a.lse = lse;
+  a.stats = static_cast<float *>(ws); a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + stat);
+  a.table = p->table; a.seq_lens = seq_lens; a.table_stride = p->table_stride;
+  // an axis of one entry has no stride
+  a.k_page = p->n_pages > 1 ? p->k_page_stride * eb : 0; a.k_tok = p->k_tok_stride * eb; a.k_head = p->kv_heads > 1 ? p->k_head_stride * eb : 0;
+  a.v_page = p->n_pages > 1 ? p->v_page_stride * eb : 0; a.v_tok = p->v_tok_stride * eb; a.v_head = p->kv_heads > 1 ? p->v_head_stride * eb : 0;
+  a.q_tok = p->batch > 1 ? q_tok_stride * eb : 0; a.q_head = p->heads > 1 ? q_head_stride * eb : 0;
+  a.o_tok = p->batch > 1 ? o_tok_stride * eb : 0; a.o_head = p->heads > 1 ? o_head_stride * eb : 0;
+  a.batch = p->batch; a.kv_heads = p->kv_heads; a.group = p->heads / p->kv_heads; a.q_blocks = (a.group + PA_MAX_Q - 1) / PA_MAX_Q;
+  a.n_pages = p->n_pages; a.lg = log2_of(p->page_tokens); a.room = p->max_pages * p->page_tokens;
+  a.n_wgs = PA_WGS; a.min_tiles = 8;
+  a.scale2 = (softmax_scale > 0.f ? softmax_scale : 1.f / sqrtf((float)p->head_dim)) * PA_LOG2E;
+  const int bound = max_seq_tokens > 0 && max_seq_tokens < a.room ? max_seq_tokens : a.room;
+  const bool whole = bound <= PA_WHOLE_TOKENS;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e;
+  if (p->dtype == LIGHTKV_BF16)
+    e = p->head_dim == 128 ? pa_launch<bf16_t, 128>(a, whole, s) : p->head_dim == 64 ? pa_launch<bf16_t, 64>(a, whole, s) : pa_launch<bf16_t, 32>(a, whole, s);
+  else
+    e = p->head_dim == 128 ? pa_launch<float, 128>(a, whole, s) : p->head_dim == 64 ? pa_launch<float, 64>(a, whole, s) : pa_launch<float, 32>(a, whole, s);
+  return e == hipSuccess ? LIGHTKV_OK : LIGHTKV_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,74 @@
+// What the calls of the paged cache share on the host: checks of the descriptor.
+#pragma once
+#include "../../include/lightkv.h"
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace lk {
+
+constexpr int PAGE_MIN_TOKENS = 8, PAGE_MAX_TOKENS = 1024;
+
+inline bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+inline bool ints_ok(const void *p) { return p && aligned_to(p, 4); }
+inline int log2_of(int v) { int l = 0; while ((1 << l) < v) ++l; return l; }
+
+// Sizes and table.
+inline lightkv_status check_page_table(const lightkv_pages *p) {
+  if (!p || !p->table) return LIGHTKV_ERR_NULL;
+  if (p->batch < 1 || p->n_pages < 1 || p->max_pages < 1 || p->page_tokens < 1 || p->table_stride < p->max_pages) return LIGHTKV_ERR_SHAPE;
+  if (!aligned_to(p->table, 4) || p->batch > LIGHTKV_PAGED_MAX_BATCH) return LIGHTKV_ERR_UNSUPPORTED;
+  if (p->page_tokens < PAGE_MIN_TOKENS || p->page_tokens > PAGE_MAX_TOKENS || (p->page_tokens & (p->page_tokens - 1))) return LIGHTKV_ERR_UNSUPPORTED;
+  if ((int64_t)p->n_pages * p->page_tokens >= (1ll << 31) || (int64_t)p->max_pages * p->page_tokens >= (1ll << 31)) return LIGHTKV_ERR_UNSUPPORTED;
+  return LIGHTKV_OK;
+}
+
+inline int page_elem_bytes(const lightkv_pages *p) { return p->dtype == LIGHTKV_BF16 ? 2 : 4; }
+
+// Rows [.., heads, head_dim] at `base`: 16-byte pieces.  An axis of one entry has no stride to speak of.
+inline lightkv_status check_strided(const void *base, int elem_bytes, int64_t outer, int64_t n_outer, int64_t head, int heads) {
+  const int per = 16 / elem_bytes;
+  if (!aligned_to(base, 16)) return LIGHTKV_ERR_UNSUPPORTED;
+  if ((n_outer > 1 && outer < 0) || (heads > 1 && head < 0)) return LIGHTKV_ERR_SHAPE;
+  if ((n_outer > 1 && outer % per) || (heads > 1 && head % per)) return LIGHTKV_ERR_UNSUPPORTED;
+  return LIGHTKV_OK;
+}
+
+// Bytes from the first element of [n_outer, heads, head_dim] to behind its last one.
+inline uint64_t strided_bytes(int elem_bytes, int64_t outer, int64_t n_outer, int64_t head, int heads, int head_dim) {
+  if (n_outer < 1) return 0;
+  return ((uint64_t)(n_outer > 1 ? outer : 0) * (uint64_t)(n_outer - 1) + (uint64_t)(heads > 1 ? head : 0) * (uint64_t)(heads - 1) + (uint64_t)head_dim) * (uint64_t)elem_bytes;
+}
+
+inline bool overlap(const void *a, uint64_t na, const void *b, uint64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + nb && y < x + na;
+}
+
+// Head sizes, type and pools (either may be missing where need_both is false).
+inline lightkv_status check_page_pools(const lightkv_pages *p, bool need_both) {
+  const lightkv_status st = check_page_table(p);
+  if (st != LIGHTKV_OK) return st;
+  if (need_both && (!p->K || !p->V)) return LIGHTKV_ERR_NULL;
+  if (p->kv_heads < 1 || p->heads < 1 || p->heads % p->kv_heads) return LIGHTKV_ERR_SHAPE;
+  if (p->dtype != LIGHTKV_F32 && p->dtype != LIGHTKV_BF16) return LIGHTKV_ERR_UNSUPPORTED;
+  if (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) return LIGHTKV_ERR_UNSUPPORTED;
+  if (p->heads > 65535) return LIGHTKV_ERR_UNSUPPORTED;
+  const int eb = page_elem_bytes(p);
+  const void *pool[2] = {p->K, p->V};
+  const int64_t pages[2] = {p->k_page_stride, p->v_page_stride}, toks[2] = {p->k_tok_stride, p->v_tok_stride}, heads[2] = {p->k_head_stride, p->v_head_stride};
+  for (int i = 0; i < 2; ++i) {
+    if (!pool[i]) continue;
+    lightkv_status s = check_strided(pool[i], eb, pages[i], p->n_pages, heads[i], p->kv_heads);
+    if (s == LIGHTKV_OK) s = check_strided(pool[i], eb, toks[i], p->page_tokens, heads[i], p->kv_heads);
+    if (s != LIGHTKV_OK) return s;
+  }
+  return LIGHTKV_OK;
+}
+
+inline uint64_t pool_bytes(const lightkv_pages *p, int64_t page_stride, int64_t tok_stride, int64_t head_stride) {
+  return strided_bytes(page_elem_bytes(p), page_stride, p->n_pages, head_stride, p->kv_heads, p->head_dim)
+         + (uint64_t)tok_stride * (uint64_t)(p->page_tokens - 1) * (uint64_t)page_elem_bytes(p);
+}
+
+}  // namespace lk

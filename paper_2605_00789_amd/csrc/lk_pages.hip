@@ -1,0 +1,356 @@
+// Tables of a paged K/V cache, built on the device from sequence lengths, and the rows that go into its pages.
+//
+// Pages and slots (lightkv_page_alloc).  With L = seq_lens, n = new tokens, P = page_tokens:
+//   need_b = ceil((L_b + n_b) / P) - ceil(L_b / P),  queue_b = sum_{b' < b} need_b',
+//   page j of sequence b, j >= ceil(L_b / P), is free_pages[count - 1 - (queue_b + j - ceil(L_b / P))],
+//   slot of the token at position x = table[b][x / P] * P + x % P.
+// The only dependence between sequences is the running sum over at most 4096 small numbers.  It is taken again by every
+// workgroup, in LDS: one trip to memory and one scan, where a launch that leaves it in memory for a second one would cost
+// the second launch and the same trip.  A page that is handed out begins with a new token, so the thread that makes that token's
+// slot also writes the table entry and nothing has to be scattered separately.
+#include "lk_common.h"
+#include "lk_pages.h"
+
+namespace lk {
+
+constexpr int PG_THREADS = 256;
+constexpr int PG_SLOTS_PER_THREAD = 4;     // one 16-byte store
+constexpr int PG_MAX_WGS = 512;
+constexpr int PG_SAT = 1 << 29;            // sums of impossible lengths stop here: above any number of pages
+
+struct AllocArgs {
+  const int32_t *cu_new, *seq_lens, *free_pages, *free_count;
+  int32_t *table, *seq_lens_out, *free_count_out, *slots, *status;
+  int64_t table_stride, slot_rows;
+  int batch, max_pages, n_pages, lg;
+  int what;   // 1: slots and table, 2: lengths, count and status
+};
+
+__device__ __forceinline__ int sat_add(int a, int b) { const int s = a + b; return s < PG_SAT ? s : PG_SAT; }
+
+// Exclusive running sum (saturating) of one number per thread over the workgroup; *total is the sum of all.
+__device__ __forceinline__ int wg_exclusive_sum(int v, int *scratch, int *total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int incl = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl = sat_add(incl, u);
+  }
+  if (lane == 63) scratch[wave] = incl;
+  __syncthreads();
+  int base = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < PG_THREADS / 64; ++w) {
+    if (w < wave) base = sat_add(base, scratch[w]);
+    sum = sat_add(sum, scratch[w]);
+  }
+  *total = sum;
+  const int before = __shfl_up(incl, 1, 64);
+  return lane == 0 ? base : sat_add(base, before);
+}
+
+// Last index i in [0, n) with list[i] <= v (list ascending, list[0] <= v).
+__device__ __forceinline__ int last_not_above(const int *list, int n, int v) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (list[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ int clamped_count(const int32_t *count, int n_pages) {
+  const int c = count[0];
+  return c < 0 ? 0 : (c > n_pages ? n_pages : c);
+}
+
+// LDS: cu [batch + 1], length [batch], queue place [batch] (-1: refused)
+__global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
+  fetch_args<AllocArgs>();
+  extern __shared__ int pg_lds[];
+  __shared__ int scratch[PG_THREADS / 64];
+  __shared__ int popped;
+  int *cu = pg_lds, *len = cu + g.batch + 1, *place = len + g.batch;
+  const int tid = threadIdx.x, count = clamped_count(g.free_count, g.n_pages);
+  const int room = g.max_pages << g.lg, P = 1 << g.lg;
+  const int per = (g.batch + PG_THREADS - 1) / PG_THREADS, b0 = tid * per, b1 = b0 + per < g.batch ? b0 + per : g.batch;
+  if (tid == 0) { popped = 0; cu[g.batch] = g.cu_new[g.batch]; }
+  int mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int first = g.cu_new[b], end = g.cu_new[b + 1], L = g.seq_lens[b];
+    cu[b] = first;
+    len[b] = L;
+    // (differences of any two ints: 64 bits)
+    const int64_t n = (int64_t)end - first;
+    const bool over = first < 0 || n < 0 || end > g.slot_rows || L < 0 || L + n > room;
+    const int need = over ? 0 : ((int)(L + n + P - 1) >> g.lg) - ((L + P - 1) >> g.lg);
+    place[b] = over ? -2 : need;
+    mine = sat_add(mine, need);
+  }
+  int total;
+  int at = wg_exclusive_sum(mine, scratch, &total);
+  for (int b = b0; b < b1; ++b) {
+    const int need = place[b];
+    if (need < 0) continue;
+    const bool ok = need == 0 || sat_add(at, need) <= count;
+    place[b] = ok ? at : -1;
+    at = sat_add(at, need);
+    if (ok && need > 0) atomicMax(&popped, at);
+  }
+  __syncthreads();
+  if ((g.what & 2) && blockIdx.x == 0) {
+    for (int b = tid; b < g.batch; b += PG_THREADS) {
+      const int p = place[b];
+      g.seq_lens_out[b] = p >= 0 ? len[b] + (cu[b + 1] - cu[b]) : len[b];
+      if (g.status) g.status[b] = p >= 0 ? 0 : (p == -1 ? 1 : 2);
+    }
+    if (tid == 0) g.free_count_out[0] = count - popped;
+  }
+  if (!(g.what & 1)) return;
+  const int64_t end = cu[g.batch] < g.slot_rows ? cu[g.batch] : g.slot_rows;
+  const int64_t step = (int64_t)gridDim.x * PG_THREADS * PG_SLOTS_PER_THREAD;
+  const bool wide = (reinterpret_cast<uintptr_t>(g.slots) & 15) == 0;
+  for (int64_t t0 = ((int64_t)blockIdx.x * PG_THREADS + tid) * PG_SLOTS_PER_THREAD; t0 < end; t0 += step) {
+    int b = 0, out[PG_SLOTS_PER_THREAD];
+    unsigned have = 0;
+    if (cu[0] <= t0) b = last_not_above(cu, g.batch, (int)t0);
+#pragma unroll
+    for (int i = 0; i < PG_SLOTS_PER_THREAD; ++i) {
+      const int64_t t = t0 + i;
+      out[i] = -1;
+      if (t >= end) continue;
+      while (b + 1 < g.batch && t >= cu[b + 1]) ++b;
+      if (t < cu[b] || t >= cu[b + 1]) continue;   // a row no sequence owns
+      have |= 1u << i;
+      if (place[b] < 0) continue;
+      const int L = len[b], pos = L + (int)(t - cu[b]), j = pos >> g.lg, old = (L + P - 1) >> g.lg;
+      int page;
+      if (j < old) {
+        page = g.table[(int64_t)b * g.table_stride + j];
+      } else {
+        page = g.free_pages[count - 1 - (place[b] + j - old)];
+        if ((pos & (P - 1)) == 0) g.table[(int64_t)b * g.table_stride + j] = page;
+      }
+      if ((unsigned)page < (unsigned)g.n_pages) out[i] = (page << g.lg) + (pos & (P - 1));
+    }
+    if (wide && have == (1u << PG_SLOTS_PER_THREAD) - 1) {
+      *reinterpret_cast<int4 *>(g.slots + t0) = int4{out[0], out[1], out[2], out[3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < PG_SLOTS_PER_THREAD; ++i)
+        if (have & (1u << i)) g.slots[t0 + i] = out[i];
+    }
+  }
+}
+
+struct FreeArgs {
+  const int32_t *done, *seq_lens, *free_count, *table;
+  int32_t *free_pages, *seq_lens_out, *free_count_out;
+  int64_t table_stride;
+  int batch, max_pages, n_pages, lg;
+  int what;   // 1: the stack, 2: lengths and count
+};
+
+// LDS: pages pushed before sequence b [batch]
+__global__ __launch_bounds__(PG_THREADS) void page_free_kernel(FreeArgs g) {
+  fetch_args<FreeArgs>();
+  extern __shared__ int pg_lds[];
+  __shared__ int scratch[PG_THREADS / 64];
+  int *before = pg_lds;
+  const int tid = threadIdx.x, count = clamped_count(g.free_count, g.n_pages), P = 1 << g.lg;
+  const int per = (g.batch + PG_THREADS - 1) / PG_THREADS, b0 = tid * per, b1 = b0 + per < g.batch ? b0 + per : g.batch;
+  int mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int L = g.seq_lens[b];
+    int held = 0;
+    if (g.done[b] != 0 && L > 0) {
+      held = (int)(((int64_t)L + P - 1) >> g.lg);
+      held = held < g.max_pages ? held : g.max_pages;
+    }
+    before[b] = held;
+    mine = sat_add(mine, held);
+  }
+  int total;
+  int at = wg_exclusive_sum(mine, scratch, &total);
+  for (int b = b0; b < b1; ++b) {
+    const int held = before[b];
+    before[b] = at;
+    at = sat_add(at, held);
+  }
+  __syncthreads();
+  const int room = g.n_pages - count, pushed = total < room ? total : room;
+  if ((g.what & 2) && blockIdx.x == 0) {
+    for (int b = tid; b < g.batch; b += PG_THREADS) g.seq_lens_out[b] = g.done[b] != 0 ? 0 : g.seq_lens[b];
+    if (tid == 0) g.free_count_out[0] = count + pushed;
+  }
+  if (!(g.what & 1)) return;
+  for (int k = blockIdx.x * PG_THREADS + tid; k < pushed; k += gridDim.x * PG_THREADS) {
+    const int b = last_not_above(before, g.batch, k);
+    g.free_pages[count + k] = g.table[(int64_t)b * g.table_stride + (k - before[b])];
+  }
+}
+
+// Rows into pages: both streams of rows are read and written once, so the time is that of a copy.  A workgroup takes whole rows
+// of K (blockIdx.y 0) or V (1), 16 bytes a thread and trip.
+struct WriteArgs {
+  const int32_t *cu_new, *slots;
+  const char *src[2];
+  char *dst[2];
+  int64_t src_tok[2], src_head[2];               // bytes
+  int64_t dst_page[2], dst_tok[2], dst_head[2];
+  int64_t rows;
+  int batch, n_slots, lg, pieces_per_row, lg_pieces;   // pieces of 16 bytes in a row, log2 of those in a head
+  int rows_per_wg;
+};
+
+__global__ __launch_bounds__(PG_THREADS) void page_write_kernel(WriteArgs g) {
+  fetch_args<WriteArgs>();
+  const int y = blockIdx.y;
+  int64_t rows = g.rows;
+  if (g.cu_new) { const int n = g.cu_new[g.batch]; rows = n < rows ? n : rows; }
+  const int per = g.pieces_per_row, in_head = (1 << g.lg_pieces) - 1;
+  for (int64_t r0 = (int64_t)blockIdx.x * g.rows_per_wg; r0 < rows; r0 += (int64_t)gridDim.x * g.rows_per_wg) {
+    const int n_rows = rows - r0 < g.rows_per_wg ? (int)(rows - r0) : g.rows_per_wg;
+    for (int i = threadIdx.x; i < n_rows * per; i += PG_THREADS) {
+      const int r = i / per, piece = i - r * per, head = piece >> g.lg_pieces;
+      const int slot = g.slots[r0 + r];
+      if ((unsigned)slot >= (unsigned)g.n_slots) continue;
+      const uint4 v = ld16(g.src[y] + (r0 + r) * g.src_tok[y] + head * g.src_head[y] + (piece & in_head) * 16);
+      char *to = g.dst[y] + (int64_t)(slot >> g.lg) * g.dst_page[y] + (int64_t)(slot & ((1 << g.lg) - 1)) * g.dst_tok[y] + head * g.dst_head[y] + (piece & in_head) * 16;
+      *reinterpret_cast<uint4 *>(to) = v;
+    }
+  }
+}
+
+}  // namespace lk
+
+using namespace lk;
+
+extern "C" {
+
+lightkv_status lightkv_page_alloc(const lightkv_pages *p, const int32_t *cu_new, const int32_t *seq_lens,
+                                  const int32_t *free_pages, const int32_t *free_count, int32_t *seq_lens_out,
+                                  int32_t *free_count_out, int32_t *slots, int64_t slot_rows, int32_t *status,
+                                  void *stream) {
+  const lightkv_status st = check_page_table(p);
+  if (st != LIGHTKV_OK) return st;
+  if (!cu_new || !seq_lens || !free_pages || !free_count || !seq_lens_out || !free_count_out || !slots) return LIGHTKV_ERR_NULL;
+  if (slot_rows < 0) return LIGHTKV_ERR_SHAPE;
+  if (slot_rows >= (1ll << 31)) return LIGHTKV_ERR_UNSUPPORTED;
+  const void *all[] = {cu_new, seq_lens, free_pages, free_count, seq_lens_out, free_count_out, slots, status};
+  for (const void *q : all)
+    if (!aligned_to(q, 4)) return LIGHTKV_ERR_UNSUPPORTED;
+  const uint64_t nb = (uint64_t)p->batch * 4, np = (uint64_t)p->n_pages * 4, nt = ((uint64_t)p->table_stride * (p->batch - 1) + p->max_pages) * 4;
+  struct Range { const void *at; uint64_t bytes; };
+  const Range in[] = {{cu_new, nb + 4}, {seq_lens, nb}, {free_pages, np}, {free_count, 4}};
+  const Range out[] = {{p->table, nt}, {slots, (uint64_t)slot_rows * 4}, {seq_lens_out, nb}, {free_count_out, 4}, {status, nb}};
+  for (int i = 0; i < 5; ++i) {
+    for (const Range &r : in) {
+      if (r.at == out[i].at && ((r.at == seq_lens && i == 2) || (r.at == free_count && i == 3))) continue;
+      if (overlap(r.at, r.bytes, out[i].at, out[i].bytes)) return LIGHTKV_ERR_SHAPE;
+    }
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[j].at, out[j].bytes, out[i].at, out[i].bytes)) return LIGHTKV_ERR_SHAPE;
+  }
+  AllocArgs g{};
+  g.cu_new = cu_new; g.seq_lens = seq_lens; g.free_pages = free_pages; g.free_count = free_count; g.table = p->table;
+  g.seq_lens_out = seq_lens_out; g.free_count_out = free_count_out; g.slots = slots; g.status = status;
+  g.table_stride = p->table_stride; g.slot_rows = slot_rows; g.batch = p->batch; g.max_pages = p->max_pages;
+  g.n_pages = p->n_pages; g.lg = log2_of(p->page_tokens);
+  const size_t lds = (3 * (size_t)p->batch + 1) * sizeof(int);
+  const int64_t per_wg = PG_THREADS * PG_SLOTS_PER_THREAD, want = (slot_rows + per_wg - 1) / per_wg;
+  const int wgs = (int)(want < 1 ? 1 : (want > PG_MAX_WGS ? PG_MAX_WGS : want));
+  // lengths and count may be written in place: then only behind the workgroups that still read them
+  const bool in_place = seq_lens_out == seq_lens || free_count_out == free_count;
+  g.what = wgs > 1 && in_place ? 1 : 3;
+  hipLaunchKernelGGL(page_alloc_kernel, dim3(wgs), dim3(PG_THREADS), lds, static_cast<hipStream_t>(stream), g);
+  if (g.what == 1) {
+    if (hipGetLastError() != hipSuccess) return LIGHTKV_ERR_LAUNCH;
+    g.what = 2;
+    hipLaunchKernelGGL(page_alloc_kernel, dim3(1), dim3(PG_THREADS), lds, static_cast<hipStream_t>(stream), g);
+  }
+  return hipGetLastError() == hipSuccess ? LIGHTKV_OK : LIGHTKV_ERR_LAUNCH;
+}
+
+lightkv_status lightkv_page_free(const lightkv_pages *p, const int32_t *done, const int32_t *seq_lens, int32_t *free_pages,
+                                 const int32_t *free_count, int32_t *seq_lens_out, int32_t *free_count_out, void *stream) {
+  const lightkv_status st = check_page_table(p);
+  if (st != LIGHTKV_OK) return st;
+  if (!done || !seq_lens || !free_pages || !free_count || !seq_lens_out || !free_count_out) return LIGHTKV_ERR_NULL;
+  const void *all[] = {done, seq_lens, free_pages, free_count, seq_lens_out, free_count_out};
+  for (const void *q : all)
+    if (!aligned_to(q, 4)) return LIGHTKV_ERR_UNSUPPORTED;
+  const uint64_t nb = (uint64_t)p->batch * 4, np = (uint64_t)p->n_pages * 4, nt = ((uint64_t)p->table_stride * (p->batch - 1) + p->max_pages) * 4;
+  struct Range { const void *at; uint64_t bytes; };
+  const Range in[] = {{done, nb}, {seq_lens, nb}, {free_count, 4}, {p->table, nt}};
+  const Range out[] = {{free_pages, np}, {seq_lens_out, nb}, {free_count_out, 4}};
+  for (int i = 0; i < 3; ++i) {
+    for (const Range &r : in) {
+      if (r.at == out[i].at && ((r.at == seq_lens && i == 1) || (r.at == free_count && i == 2))) continue;
+      if (overlap(r.at, r.bytes, out[i].at, out[i].bytes)) return LIGHTKV_ERR_SHAPE;
+    }
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[j].at, out[j].bytes, out[i].at, out[i].bytes)) return LIGHTKV_ERR_SHAPE;
+  }
+  FreeArgs g{};
+  g.done = done; g.seq_lens = seq_lens; g.free_pages = free_pages; g.free_count = free_count; g.table = p->table;
+  g.seq_lens_out = seq_lens_out; g.free_count_out = free_count_out; g.table_stride = p->table_stride; g.batch = p->batch;
+  g.max_pages = p->max_pages; g.n_pages = p->n_pages; g.lg = log2_of(p->page_tokens);
+  const size_t lds = (size_t)p->batch * sizeof(int);
+  const int64_t most = (int64_t)p->batch * p->max_pages < p->n_pages ? (int64_t)p->batch * p->max_pages : p->n_pages;
+  const int64_t want = (most + PG_THREADS * 4 - 1) / (PG_THREADS * 4);
+  const int wgs = (int)(want < 1 ? 1 : (want > PG_MAX_WGS ? PG_MAX_WGS : want));
+  const bool in_place = seq_lens_out == seq_lens || free_count_out == free_count;
+  g.what = wgs > 1 && in_place ? 1 : 3;
+  hipLaunchKernelGGL(page_free_kernel, dim3(wgs), dim3(PG_THREADS), lds, static_cast<hipStream_t>(stream), g);
+  if (g.what == 1) {
+    if (hipGetLastError() != hipSuccess) return LIGHTKV_ERR_LAUNCH;
+    g.what = 2;
+    hipLaunchKernelGGL(page_free_kernel, dim3(1), dim3(PG_THREADS), lds, static_cast<hipStream_t>(stream), g);
+  }
+  return hipGetLastError() == hipSuccess ? LIGHTKV_OK : LIGHTKV_ERR_LAUNCH;
+}
+
+lightkv_status lightkv_page_write(const lightkv_pages *p, const int32_t *cu_new, const int32_t *slots, int64_t rows,
+                                  const void *K, int64_t k_tok_stride, int64_t k_head_stride,
+                                  const void *V, int64_t v_tok_stride, int64_t v_head_stride, void *stream) {
+  lightkv_status st = check_page_pools(p, false);
+  if (st != LIGHTKV_OK) return st;
+  if (!slots || (!K && !V) || (K && !p->K) || (V && !p->V)) return LIGHTKV_ERR_NULL;
+  if (rows < 0) return LIGHTKV_ERR_SHAPE;
+  if (rows >= (1ll << 31) || !aligned_to(slots, 4) || !aligned_to(cu_new, 4)) return LIGHTKV_ERR_UNSUPPORTED;
+  const int eb = page_elem_bytes(p);
+  const void *src[2] = {K, V};
+  void *dst[2] = {p->K, p->V};
+  const int64_t tok[2] = {k_tok_stride, v_tok_stride}, head[2] = {k_head_stride, v_head_stride};
+  const int64_t page_s[2] = {p->k_page_stride, p->v_page_stride}, tok_s[2] = {p->k_tok_stride, p->v_tok_stride}, head_s[2] = {p->k_head_stride, p->v_head_stride};
+  for (int i = 0; i < 2; ++i) {
+    if (!src[i]) continue;
+    st = check_strided(src[i], eb, tok[i], rows, head[i], p->kv_heads);
+    if (st != LIGHTKV_OK) return st;
+    const uint64_t n = strided_bytes(eb, tok[i], rows, head[i], p->kv_heads, p->head_dim);
+    for (int k = 0; k < 2; ++k)
+      if (src[k] && overlap(src[i], n, dst[k], pool_bytes(p, page_s[k], tok_s[k], head_s[k]))) return LIGHTKV_ERR_SHAPE;
+  }
+  if (rows == 0) return LIGHTKV_OK;
+  WriteArgs g{};
+  g.cu_new = cu_new; g.slots = slots; g.rows = rows; g.batch = p->batch; g.n_slots = p->n_pages * p->page_tokens; g.lg = log2_of(p->page_tokens);
+  int n = 0;
+  for (int i = 0; i < 2; ++i) {
+    if (!src[i]) continue;
+    g.src[n] = static_cast<const char *>(src[i]); g.dst[n] = static_cast<char *>(dst[i]);
+    g.src_tok[n] = (rows > 1 ? tok[i] : 0) * eb; g.src_head[n] = (p->kv_heads > 1 ? head[i] : 0) * eb;
+    g.dst_page[n] = (p->n_pages > 1 ? page_s[i] : 0) * eb; g.dst_tok[n] = tok_s[i] * eb; g.dst_head[n] = (p->kv_heads > 1 ? head_s[i] : 0) * eb;
+    ++n;
+  }
+  g.lg_pieces = log2_of(p->head_dim * eb / 16);
+  g.pieces_per_row = p->kv_heads << g.lg_pieces;
+  g.rows_per_wg = g.pieces_per_row < 1024 ? 1024 / g.pieces_per_row : 1;
+  const int64_t want = (rows + g.rows_per_wg - 1) / g.rows_per_wg, wgs = want < (1 << 20) ? want : (1 << 20);
+  hipLaunchKernelGGL(page_write_kernel, dim3((unsigned)wgs, (unsigned)n), dim3(PG_THREADS), 0, static_cast<hipStream_t>(stream), g);
+  return hipGetLastError() == hipSuccess ? LIGHTKV_OK : LIGHTKV_ERR_LAUNCH;
+}
+
+}  // extern "C"

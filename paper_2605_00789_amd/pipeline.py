@@ -433,3 +433,69 @@ class EdgeTopKSchedule:
             out.append(r)
             h_cu_vis, X, K, V, pos, cu_vis = r.h_cu_vis_out, r.X, r.K, r.V, r.pos, r.cu_vis_out
         return out
+
+
+class PagedCache:
+    """K/V pages of `layers` decoder layers whose sequences have the same lengths, with the table, the stack of free pages and
+    the lengths that go with them (layers in front of a compression stage and behind it hold different lengths: a cache
+    each).  Everything lives on the device and no call reads it back: append (or store_stage) makes room for new tokens,
+    write puts a layer's rows there, attend is one new token's attention, release takes back what finished sequences hold.
+    The calls only enqueue, on the current stream or `stream`, so a decoding step can be captured into a graph and replayed.
+
+    pools: one (K, V) pair per layer, stored head-major inside a page ([n_pages, kv_heads, page_tokens, head_dim]: a head's
+    rows of a page are one run of memory) and handed out as [n_pages, page_tokens, kv_heads, head_dim] views."""
+
+    def __init__(self, *, dtype: str, batch: int, heads: int, head_dim: int, n_pages: int, max_seq_tokens: int,
+                 max_new_tokens: int, kv_heads: Optional[int] = None, page_tokens: int = 16, layers: int = 1, device="cuda:0"):
+        self.device = torch.device(device)
+        i32 = dict(dtype=torch.int32, device=self.device)
+        tdtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        kv_heads = heads if kv_heads is None else kv_heads
+        self.batch, self.max_seq_tokens = batch, max_seq_tokens
+        self.table = torch.zeros(batch, -(-max_seq_tokens // page_tokens), **i32)
+        self.seq_lens = torch.zeros(batch, **i32)
+        self.status = torch.zeros(batch, **i32)
+        self.free_pages = torch.arange(n_pages - 1, -1, -1, **i32)
+        self.free_count = torch.full((1,), n_pages, **i32)
+        self.slots = torch.full((max_new_tokens,), -1, **i32)
+        self.pools, self.pages = [], []
+        for _ in range(layers):
+            # (zeros: a page's rows behind its last token are loaded, if not used)
+            K, V = (torch.zeros(n_pages, kv_heads, page_tokens, head_dim, dtype=tdtype, device=self.device).transpose(1, 2)
+                    for _ in range(2))
+            self.pools.append((K, V))
+            self.pages.append(B.Pages(self.table, K=K, V=V, heads=heads))
+        self._cu_new = torch.arange(batch + 1, **i32)
+        self.one_each = self._cu_new              # cu_new of a decoding step: one token for every sequence
+        self.ws = torch.empty(B.lightkv_page_attention_workspace(self.pages[0]), dtype=torch.uint8, device=self.device)
+
+    def append(self, cu_new: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Room for cu_new[b + 1] - cu_new[b] more tokens of every sequence (None: one each); the write calls that follow
+        fill it.  Returns `status` (device, see lightkv_page_alloc), which is the caller's to look at."""
+        self._cu_new = self.one_each if cu_new is None else cu_new
+        B.lightkv_page_alloc(self.pages[0], self._cu_new, self.seq_lens, self.free_pages, self.free_count, self.seq_lens,
+                             self.free_count, self.slots, status=self.status, stream=stream)
+        return self.status
+
+    def write(self, layer: int, K: torch.Tensor, V: torch.Tensor, stream=None):
+        """A layer's rows [tokens, kv_heads, head_dim] (or [tokens, kv_heads * head_dim]) of the last append."""
+        B.lightkv_page_write(self.pages[layer], self.slots, K, V, cu_new=self._cu_new, stream=stream)
+
+    def store_stage(self, layer: int, st, stream=None) -> torch.Tensor:
+        """append and write of what a compression stage leaves (StageBuffers, or the EdgeStepResult of a schedule whose
+        counts depend on the data): the lengths are taken from its cu_vis_out on the device."""
+        K, V = (st.K_out, st.V_out) if isinstance(st, StageBuffers) else (st.K, st.V)
+        status = self.append(st.cu_vis_out, stream=stream)
+        self.write(layer, K, V, stream=stream)
+        return status
+
+    def attend(self, layer: int, Q: torch.Tensor, out: torch.Tensor, *, lse=None, softmax_scale: float = 0.0, stream=None):
+        """out[b] = attention of query Q[b] over the tokens sequence b holds in this layer."""
+        B.lightkv_page_attention(self.pages[layer], self.seq_lens, Q, out, self.ws, lse=lse, softmax_scale=softmax_scale,
+                                 max_seq_tokens=self.max_seq_tokens, stream=stream)
+        return out
+
+    def release(self, done: torch.Tensor, stream=None):
+        """Pages of every sequence with done[b] != 0 (int32, device) go back; its length becomes zero."""
+        B.lightkv_page_free(self.pages[0], done, self.seq_lens, self.free_pages, self.free_count, self.seq_lens,
+                            self.free_count, stream=stream)

@@ -1,0 +1,150 @@
+"""The calls of the paged cache refuse bad arguments on the host, before anything is launched (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+OK, NULL, SHAPE, UNSUPPORTED, WORKSPACE = 0, 1, 2, 5, 6
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2605_00789_amd import binding
+    return binding
+
+
+def at(k):
+    """Made-up device addresses far apart: only host-side validation may look at them."""
+    return 0x10000000 * (k + 1)
+
+
+def _pages(B, **over):
+    p = B._CPages()
+    p.batch, p.n_pages, p.page_tokens, p.max_pages, p.table_stride, p.table = 3, 10, 16, 4, 4, at(0)
+    p.heads, p.kv_heads, p.head_dim, p.dtype, p.K, p.V = 8, 2, 64, 1, at(1), at(2)
+    p.k_page_stride, p.k_tok_stride, p.k_head_stride = 16 * 128, 128, 64
+    p.v_page_stride, p.v_tok_stride, p.v_head_stride = 16 * 128, 64, 16 * 64
+    for k, v in over.items():
+        setattr(p, k, v)
+    return p
+
+
+TABLE = [
+    (dict(table=None), NULL), (dict(batch=0), SHAPE), (dict(n_pages=0), SHAPE), (dict(max_pages=0), SHAPE), (dict(page_tokens=0), SHAPE),
+    (dict(table_stride=3), SHAPE), (dict(table=at(0) + 2), UNSUPPORTED), (dict(batch=4097), UNSUPPORTED),
+    (dict(page_tokens=4), UNSUPPORTED), (dict(page_tokens=24), UNSUPPORTED), (dict(page_tokens=2048), UNSUPPORTED),
+    (dict(n_pages=1 << 27, page_tokens=16), UNSUPPORTED), (dict(max_pages=1 << 27, table_stride=1 << 27), UNSUPPORTED),
+]
+POOLS = TABLE + [
+    (dict(kv_heads=0), SHAPE), (dict(heads=0), SHAPE), (dict(heads=7), SHAPE), (dict(head_dim=48), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED),
+    (dict(dtype=2), UNSUPPORTED), (dict(heads=1 << 17), UNSUPPORTED), (dict(K=at(1) + 8), UNSUPPORTED),
+    (dict(k_page_stride=-128), SHAPE), (dict(v_tok_stride=-64), SHAPE), (dict(k_head_stride=-64), SHAPE),
+    (dict(k_tok_stride=60), UNSUPPORTED), (dict(v_head_stride=68), UNSUPPORTED), (dict(v_page_stride=1001), UNSUPPORTED),
+]
+
+
+def _alloc(B, p, **o):
+    a = dict(cu=at(3), lens=at(4), free=at(5), count=at(6), lens_out=at(7), count_out=at(8), slots=at(9), rows=50, status=at(10))
+    a.update(o)
+    return B._lib.lightkv_page_alloc(C.byref(p) if p is not None else None, a["cu"], a["lens"], a["free"], a["count"], a["lens_out"],
+                                     a["count_out"], a["slots"], a["rows"], a["status"], None)
+
+
+def _free(B, p, **o):
+    a = dict(done=at(3), lens=at(4), free=at(5), count=at(6), lens_out=at(7), count_out=at(8))
+    a.update(o)
+    return B._lib.lightkv_page_free(C.byref(p) if p is not None else None, a["done"], a["lens"], a["free"], a["count"], a["lens_out"], a["count_out"], None)
+
+
+def _write(B, p, **o):
+    a = dict(cu=at(3), slots=at(4), rows=50, K=at(5), kt=128, kh=64, V=at(6), vt=128, vh=64)
+    a.update(o)
+    return B._lib.lightkv_page_write(C.byref(p) if p is not None else None, a["cu"], a["slots"], a["rows"], a["K"], a["kt"], a["kh"], a["V"], a["vt"], a["vh"], None)
+
+
+def _attend(B, p, **o):
+    a = dict(lens=at(3), bound=0, Q=at(4), qt=512, qh=64, scale=0.0, out=at(5), ot=512, oh=64, lse=at(6), ws=at(7), bytes=1 << 30)
+    a.update(o)
+    return B._lib.lightkv_page_attention(C.byref(p) if p is not None else None, a["lens"], a["bound"], a["Q"], a["qt"], a["qh"], a["scale"], a["out"],
+                                         a["ot"], a["oh"], a["lse"], a["ws"], a["bytes"], None)
+
+
+@pytest.mark.parametrize("over,want", TABLE)
+def test_tables(B, over, want):
+    assert _alloc(B, _pages(B, **over)) == want
+    assert _free(B, _pages(B, **over)) == want
+
+
+@pytest.mark.parametrize("over,want", POOLS)
+def test_pools(B, over, want):
+    assert _write(B, _pages(B, **over)) == want
+    assert _attend(B, _pages(B, **over)) == want
+    n = C.c_size_t(0)
+    assert B._lib.lightkv_page_attention_workspace(C.byref(_pages(B, **over)), C.byref(n)) == want
+
+
+def test_descriptor_is_required(B):
+    assert _alloc(B, None) == NULL and _free(B, None) == NULL and _write(B, None) == NULL and _attend(B, None) == NULL
+    assert B._lib.lightkv_page_attention_workspace(None, C.byref(C.c_size_t(0))) == NULL
+    assert B._lib.lightkv_page_attention_workspace(C.byref(_pages(B)), None) == NULL
+
+
+def test_alloc_arguments(B):
+    p = _pages(B)
+    for name in ("cu", "lens", "free", "count", "lens_out", "count_out", "slots"):
+        assert _alloc(B, p, **{name: None}) == NULL, name
+        assert _alloc(B, p, **{name: at(20) + 2}) == UNSUPPORTED, name
+    assert _alloc(B, p, rows=-1) == SHAPE and _alloc(B, p, rows=1 << 31) == UNSUPPORTED
+    # outputs may not lie in inputs or in each other; lengths and count may be updated in place, but not half
+    assert _alloc(B, p, slots=at(3)) == SHAPE and _alloc(B, p, slots=at(0) + 8) == SHAPE and _alloc(B, p, status=at(9) + 4) == SHAPE
+    assert _alloc(B, p, lens_out=at(4) + 4) == SHAPE and _alloc(B, p, lens_out=at(3)) == SHAPE
+    assert _alloc(B, p, count_out=at(5) + 36) == SHAPE and _alloc(B, p, slots=at(5)) == SHAPE
+    assert _alloc(B, p, lens_out=at(6)) == SHAPE      # the length array over the count
+
+
+def test_free_arguments(B):
+    p = _pages(B)
+    for name in ("done", "lens", "free", "count", "lens_out", "count_out"):
+        assert _free(B, p, **{name: None}) == NULL, name
+        assert _free(B, p, **{name: at(20) + 1}) == UNSUPPORTED, name
+    assert _free(B, p, free=at(0)) == SHAPE and _free(B, p, lens_out=at(3)) == SHAPE and _free(B, p, lens_out=at(4) + 4) == SHAPE
+    assert _free(B, p, count_out=at(5)) == SHAPE and _free(B, p, free=at(4)) == SHAPE
+
+
+def test_write_arguments(B):
+    p = _pages(B)
+    assert _write(B, p, slots=None) == NULL and _write(B, p, K=None, V=None) == NULL
+    assert _write(B, _pages(B, V=None)) == NULL                       # rows for a pool that is not there
+    assert _write(B, p, rows=-1) == SHAPE and _write(B, p, rows=1 << 31) == UNSUPPORTED
+    assert _write(B, p, rows=0) == OK
+    assert _write(B, p, K=at(5) + 4) == UNSUPPORTED and _write(B, p, kt=130) == UNSUPPORTED and _write(B, p, vh=33) == UNSUPPORTED
+    assert _write(B, p, kt=-128) == SHAPE
+    assert _write(B, p, slots=at(4) + 1) == UNSUPPORTED and _write(B, p, cu=at(3) + 2) == UNSUPPORTED
+    assert _write(B, p, K=at(1) + 256) == SHAPE and _write(B, p, V=at(1)) == SHAPE and _write(B, p, K=at(2) + 10 * 16 * 256 - 32) == SHAPE
+
+
+def test_attention_arguments(B):
+    p = _pages(B)
+    for name in ("lens", "Q", "out"):
+        assert _attend(B, p, **{name: None}) == NULL, name
+    assert _attend(B, _pages(B, V=None)) == NULL
+    for bad in (-1.0, float("nan"), float("inf")):
+        assert _attend(B, p, scale=bad) == SHAPE
+    assert _attend(B, p, bound=-1) == SHAPE
+    assert _attend(B, p, Q=at(4) + 8) == UNSUPPORTED and _attend(B, p, qt=509) == UNSUPPORTED and _attend(B, p, oh=68) == UNSUPPORTED
+    assert _attend(B, p, lens=at(3) + 2) == UNSUPPORTED and _attend(B, p, lse=at(6) + 2) == UNSUPPORTED
+    assert _attend(B, p, out=at(4)) == SHAPE and _attend(B, p, out=at(4) + 512) == SHAPE and _attend(B, p, lse=at(5) + 64) == SHAPE
+    assert _attend(B, p, oh=32) == SHAPE and _attend(B, p, ot=0) == SHAPE              # rows of the output in each other
+    n = C.c_size_t(0)
+    assert B._lib.lightkv_page_attention_workspace(C.byref(p), C.byref(n)) == OK and n.value > 0
+    assert _attend(B, p, ws=None) == WORKSPACE and _attend(B, p, ws=at(7) + 16) == WORKSPACE and _attend(B, p, bytes=n.value - 1) == WORKSPACE
+    # tiles of all rows of the table are counted in 32 bits
+    wide = _pages(B, batch=4096, max_pages=1 << 24, table_stride=1 << 24)
+    assert _attend(B, wide) == UNSUPPORTED
+
+
+def test_binding_refuses_host_tensors(B):
+    import torch
+    with pytest.raises(ValueError):
+        B.Pages(torch.zeros(2, 2, dtype=torch.int32), n_pages=4, page_tokens=16)
+    with pytest.raises(ValueError):
+        B.Pages(torch.zeros(2, 2), n_pages=4, page_tokens=16)
