@@ -354,6 +354,17 @@ __device__ __forceinline__ PaCut pa_cut(const PageAttnArgs &a, int tile, int seg
   return c;
 }
 
+// The sequence that tile `at` of the line lies in (at < all tiles).
+__device__ __forceinline__ int pa_sequence(const PageAttnArgs &a, const int *before, int segs, int64_t at) {
+  int lo = 0, hi = a.batch;    // last sequence that begins at or before it: one with tiles, since empty ones begin where the next does
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if ((int64_t)before[mid] * segs <= at) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
 template <typename T, int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_split_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
@@ -365,15 +376,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_split_kernel(PageAttn
   int64_t at = (int64_t)blockIdx.x * c.piece;
   const int64_t end = at + c.piece < c.tiles ? at + c.piece : c.tiles;
   if (at >= end) return;
-  int lo = 0, hi = a.batch;    // last sequence that begins at or before `at`
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if ((int64_t)before[mid] * segs <= at) lo = mid;
-    else hi = mid;
-  }
-  int b = lo;
+  int b = pa_sequence(a, before, segs, at);
   while (at < end) {
-    while (before[b + 1] == before[b] || (int64_t)before[b + 1] * segs <= at) ++b;   // (ends: at < tiles)
+    while ((int64_t)before[b + 1] * segs <= at) ++b;   // (ends: at < tiles)
     const int nt = before[b + 1] - before[b];
     const int64_t local = at - (int64_t)before[b] * segs;
     const int seg = (int)(local / nt), t0 = (int)(local - (int64_t)seg * nt);
@@ -389,39 +394,104 @@ __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_split_kernel(PageAttn
   }
 }
 
+constexpr int PA_WGS = 512;          // workgroups of a split launch: two of four waves fit a CU
 constexpr int PA_JOIN_THREADS = 256;
 
-// Joins the records of one segment, and writes what sequences without tokens get.
-template <typename T, int HD>
+// Joins the records of a segment, and writes what sequences without tokens get.  A segment that is cut belongs to the
+// workgroup of the split launch in which it begins, so there are at most n_wgs of them: BY_PIECE takes one per workgroup.
+// With fewer segments than that a workgroup takes a segment (and one query head of it, blockIdx.y, as records are many then).
+template <typename T, int HD, bool BY_PIECE>
 __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
   extern __shared__ float pa_lds[];
   __shared__ int scratch[PA_JOIN_THREADS / 64];
+  __shared__ float tops[PA_MAX_Q], sums[PA_MAX_Q];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, segs = a.kv_heads * a.q_blocks;
   int *before = reinterpret_cast<int *>(pa_lds);
   const PaCut c = pa_cut(a, PaGeo<T, HD>::TILE, segs, before, scratch);
-  const int b = blockIdx.x / segs, seg = blockIdx.x - b * segs, nt = before[b + 1] - before[b];
+  for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+    if (before[b + 1] != before[b] || blockIdx.y) continue;
+    for (int i = tid; i < a.kv_heads * a.group * HD; i += PA_JOIN_THREADS) pa_finish<T>(a, b, i / HD, i % HD, 0.f, 0.f, 0.f);
+  }
+  int b, seg, nt, w0;
+  int64_t first;
+  if (BY_PIECE) {
+    w0 = blockIdx.x;
+    const int64_t end = (int64_t)(w0 + 1) * c.piece;
+    if (end >= c.tiles) return;
+    b = pa_sequence(a, before, segs, end);
+    nt = before[b + 1] - before[b];
+    const int64_t local = end - (int64_t)before[b] * segs;
+    seg = (int)(local / nt);
+    first = (int64_t)before[b] * segs + (int64_t)seg * nt;
+    if (first == end || first < end - c.piece) return;   // cut in front of a segment; one that began earlier
+  } else {
+    b = blockIdx.x / segs; seg = blockIdx.x - b * segs;
+    nt = before[b + 1] - before[b];
+    if (nt == 0) return;
+    first = (int64_t)before[b] * segs + (int64_t)seg * nt;
+    w0 = (int)(first / c.piece);
+  }
+  const int n_rec = (int)((first + nt - 1) / c.piece) - w0 + 1;
+  if (n_rec == 1) return;    // one workgroup had it all
   const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
   const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
-  const int64_t first = (int64_t)before[b] * segs + (int64_t)seg * nt;
-  const int w0 = nt ? (int)(first / c.piece) : 0, w1 = nt ? (int)((first + nt - 1) / c.piece) : -1;
-  if (nt && w0 == w1) return;    // one workgroup had it all
-  for (int i = threadIdx.x; i < gq * HD; i += PA_JOIN_THREADS) {
-    const int n = i / HD, d = i % HD;
-    float top = -INFINITY, sum = 0.f, o = 0.f;
-    for (int w = w0; w <= w1; ++w) top = fmaxf(top, a.stats[((int64_t)(2 * w + (w == w0 ? 1 : 0)) * rows + n) * 2]);
+  const int q0 = BY_PIECE ? 0 : blockIdx.y, q1 = BY_PIECE ? gq : q0 + 1;
+  if (q0 >= gq) return;
+  const int nq = q1 - q0;
+  __syncthreads();           // (the list of sequences is overwritten)
+  float *weight = pa_lds;    // [nq][n_rec]
+  auto record = [&](int r) { return (int64_t)(2 * (w0 + r) + (r == 0 ? 1 : 0)) * rows; };
+  for (int n = wave; n < nq; n += PA_JOIN_THREADS / 64) {
+    float top = -INFINITY, sum = 0.f;
+    for (int r = lane; r < n_rec; r += 64) top = fmaxf(top, a.stats[(record(r) + q0 + n) * 2]);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     const float ref = top == -INFINITY ? 0.f : top;
-    for (int w = w0; w <= w1; ++w) {
-      const int64_t r = (int64_t)(2 * w + (w == w0 ? 1 : 0)) * rows + n;
-      const float mw = a.stats[r * 2], f = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - ref);
-      sum += f * a.stats[r * 2 + 1];
-      o += f * a.part[r * HD + d];
+    for (int r = lane; r < n_rec; r += 64) {
+      const float *s = a.stats + (record(r) + q0 + n) * 2;
+      const float f = s[0] == top ? 1.f : __builtin_amdgcn_exp2f(s[0] - ref);
+      weight[n * n_rec + r] = f;
+      sum += f * s[1];
     }
-    pa_finish<T>(a, b, h0 + n, d, top, sum, o);
+    sum = wave_sum_butterfly(sum);
+    if (lane == 0) { tops[n] = top; sums[n] = sum; }
+  }
+  __syncthreads();
+  // four elements a thread; where these are fewer than the threads, groups of threads take every n-th record
+  constexpr int V = HD / 4;
+  const int items = nq * V, groups = items < PA_JOIN_THREADS ? PA_JOIN_THREADS / items : 1;
+  float4 *part_sum = reinterpret_cast<float4 *>(pa_lds + (((size_t)nq * n_rec + 3) & ~(size_t)3));   // [groups][items]
+  for (int i0 = 0; i0 < items; i0 += PA_JOIN_THREADS) {
+    const int grp = groups > 1 ? tid / items : 0, i = groups > 1 ? tid - grp * items : i0 + tid;
+    const bool mine = grp < groups && i < items;
+    const int n = i / V, d = (i - n * V) * 4;
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+    if (mine) {
+#pragma unroll 8
+      for (int r = grp; r < n_rec; r += groups) {
+        const float4 v = *reinterpret_cast<const float4 *>(a.part + (record(r) + q0 + n) * HD + d);
+        const float f = weight[n * n_rec + r];
+        o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
+      }
+    }
+    if (groups > 1) {
+      if (mine) part_sum[grp * items + i] = o;
+      __syncthreads();
+      if (grp != 0) continue;
+      for (int k = 1; k < groups; ++k) {
+        const float4 v = part_sum[k * items + i];
+        o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+      }
+    }
+    if (!mine) continue;
+    const float e[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) pa_finish<T>(a, b, h0 + q0 + n, d + k, tops[n], sums[n], e[k]);
   }
 }
 
-constexpr int PA_WGS = 512;          // workgroups of a split launch: two of four waves fit a CU
 constexpr int PA_WHOLE_TOKENS = 1024;
 
 inline int pa_rows(const lightkv_pages *p) { const int g = p->heads / p->kv_heads; return g < PA_MAX_Q ? g : PA_MAX_Q; }
@@ -441,7 +511,11 @@ static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t strea
   hipLaunchKernelGGL((page_attn_split_kernel<T, HD, 4>), dim3(a.n_wgs), dim3(256), pa_join_floats<HD>(4, rows) * sizeof(float) + cut, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((page_attn_join_kernel<T, HD>), dim3(segs), dim3(PA_JOIN_THREADS), cut, stream, a);
+  // LDS: the list of sequences, then weights of all records and the sums of the thread groups
+  const bool by_piece = segs >= (unsigned)a.n_wgs;
+  const size_t join = ((size_t)(by_piece ? rows : 1) * (a.n_wgs + 1) + 4) * sizeof(float) + (size_t)PA_JOIN_THREADS * sizeof(float4), lds = join > cut ? join : cut;
+  if (by_piece) hipLaunchKernelGGL((page_attn_join_kernel<T, HD, true>), dim3(a.n_wgs), dim3(PA_JOIN_THREADS), lds, stream, a);
+  else hipLaunchKernelGGL((page_attn_join_kernel<T, HD, false>), dim3(segs, rows), dim3(PA_JOIN_THREADS), lds, stream, a);
   return hipGetLastError();
 }
 
