@@ -7,15 +7,15 @@
 // V bound it, at any number of query heads a K/V head serves.  So the matrix instructions are there to keep the vector units
 // out of the way: up to 16 query heads of a K/V head are the columns of one 16 x 16 block, and fewer cost the same.
 //
-// Nothing of K or V passes through LDS.  A tile is 32 tokens (16 for fp32) of one K/V head, and a lane (m = lane % 16,
-// g = lane / 16) loads
-//   K: token 16 h + m, 16-byte chunks g, g + 4, ..  = rows of the first product's A operand (S^T = K Q^T),
-//   V: tokens 16 h + 4 g + i, elements m * head_dim / 16 ..  (16 lanes read a whole row).
-// S^T leaves lane (m, g) with the scores of query m against tokens 16 h + 4 g + i: as they stand the B operand of
-// out^T = V^T P^T, since a product does not care how the tokens it sums over are numbered as long as both sides agree.  V's
-// operand wants one element of eight tokens in a lane, where a lane holds several elements of each of its eight tokens: a
-// transposition inside the lane, one byte permutation per register (fp32: none).  Output rows come out permuted, element
-// m * head_dim / 16 + t for row m of block t, which the store undoes.
+// A tile is 32 tokens (16 for fp32) of one K/V head.  Lane (m = lane % 16, g = lane / 16) of the wave that works on it
+//   - loads K and V as whole rows, the lanes of a row side by side (see pa_load),
+//   - takes K's rows from LDS, where the wave has put them, as the A operand of S^T = K Q^T: row m of half h is token
+//     8 (m / 4) + 4 h + m % 4 (fp32: token m).  S^T then leaves lane (m, g) with the scores of query m against tokens 8 g + j
+//     (4 g + j), j = 4 h + i: as they stand the B operand of out^T = V^T P^T,
+//   - has loaded elements m * head_dim / 16 .. of V's tokens 8 g + j, all of them: V's operand wants one element of the eight
+//     tokens in a lane, a transposition inside the lane, one byte permutation per register (fp32: none).  Output rows come
+//     out permuted, element m * head_dim / 16 + t for row m of block t, which the store undoes.
+// A product does not care how the things it sums over are numbered as long as both operands agree: that is what all of this uses.
 #include "lk_common.h"
 #include "lk_pages.h"
 
@@ -41,7 +41,10 @@ template <typename T, int HD> struct PaGeo {
   static constexpr int EB = Elem<T>::BYTES;
   static constexpr int TILE = EB == 2 ? 32 : 16;   // tokens
   static constexpr int NH = TILE / 16;             // 16-token halves
-  static constexpr int KL = HD * EB / 64;          // 16-byte loads per lane and K row
+  static constexpr int C = HD * EB / 16;           // 16-byte chunks of a row
+  static constexpr int KL = C / 4;                 // ... of it in one lane's operand
+  static constexpr int KI = TILE * C / 64;         // loads of K per lane and tile
+  static constexpr int K_BYTES = TILE * C * 16;
   static constexpr int NK = TILE / 4;              // V rows per lane
   static constexpr int VT = HD / 16;               // elements per lane and V row, = output blocks
   static constexpr int VW = VT * EB / 4;           // ... in words
@@ -49,24 +52,39 @@ template <typename T, int HD> struct PaGeo {
 
 template <typename T, int HD> struct PaTile {
   using G = PaGeo<T, HD>;
-  uint4 k[G::NH][G::KL];
+  uint4 k[G::KI];
   uint32_t v[G::NK][G::VW];
   uint32_t live;                                   // bit t: token t of the tile counts
 };
 
+// K and V are read once (a group of more than 16 query heads aside) and are larger than the caches: loads that do not stay
+// there leave the memory more of its rate.  131000 tokens x 8 heads, 537 MB: 97 -> 86 us; 64 ragged sequences, 979 MB: 195 -> 181.
+__device__ __forceinline__ uint4 pa_ld16(const char *p) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)));
+}
 template <int W> __device__ __forceinline__ void pa_load_words(uint32_t (&d)[W], const char *p) {
   if constexpr (W % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < W; i += 4) {
-      const uint4 v = ld16(p + i * 4);
+      const uint4 v = pa_ld16(p + i * 4);
       d[i] = v.x; d[i + 1] = v.y; d[i + 2] = v.z; d[i + 3] = v.w;
     }
   } else if constexpr (W == 2) {
-    const uint2 v = *reinterpret_cast<const uint2 *>(p);
-    d[0] = v.x; d[1] = v.y;
+    const uint64_t v = __builtin_nontemporal_load(reinterpret_cast<const uint64_t *>(p));
+    d[0] = (uint32_t)v; d[1] = (uint32_t)(v >> 32);
   } else {
-    d[0] = *reinterpret_cast<const uint32_t *>(p);
+    d[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p));
   }
+}
+
+// Row of the first product's A operand <-> token of the tile, and where a token's chunk lies in LDS: chunks are swapped by the
+// row number so that the 16 rows of an operand load lie in 16 different places of the 256 bytes a bank cycle covers.
+template <typename T, int HD> __device__ __forceinline__ int pa_token_of(int h, int m) { return PaGeo<T, HD>::NH == 2 ? (m >> 2) * 8 + h * 4 + (m & 3) : m; }
+template <typename T, int HD> __device__ __forceinline__ int pa_place(int token, int chunk) {
+  constexpr int C = PaGeo<T, HD>::C, SHIFT = C >= 16 ? 0 : (C == 8 ? 1 : 2);
+  const int m = PaGeo<T, HD>::NH == 2 ? (token >> 3) * 4 + (token & 3) : token;
+  return (token * C + (chunk ^ ((m >> SHIFT) & (C - 1)))) * 16;
 }
 
 // One wave's share of a segment: (m, l, o) of up to 16 queries.  m belongs to query lane % 16 in all four lane groups, l holds
@@ -78,21 +96,26 @@ template <typename T, int HD> struct PaState {
 };
 
 template <typename T, int HD>
-__device__ __forceinline__ void pa_accumulate(PaState<T, HD> &st, PaTile<T, HD> &tile, const uint4 (&q)[PaGeo<T, HD>::KL], float scale2, int g) {
+__device__ __forceinline__ void pa_accumulate(PaState<T, HD> &st, PaTile<T, HD> &tile, const uint4 (&q)[PaGeo<T, HD>::KL], float scale2, char *lds) {
   using G = PaGeo<T, HD>;
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  // (the wave's own piece of LDS, and a wave's LDS operations are done in order: nothing to wait for in between)
+#pragma unroll
+  for (int i = 0; i < G::KI; ++i) *reinterpret_cast<uint4 *>(lds + pa_place<T, HD>((lane / G::C) * G::KI + i, lane % G::C)) = tile.k[i];
   float s[G::NH][4];
 #pragma unroll
   for (int h = 0; h < G::NH; ++h) {
     f32x4 c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < G::KL; ++i) {
+      const uint4 k = *reinterpret_cast<const uint4 *>(lds + pa_place<T, HD>(pa_token_of<T, HD>(h, m), i * 4 + g));
       if constexpr (G::EB == 2) {
-        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, tile.k[h][i]), __builtin_bit_cast(bf16x8, q[i]), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[i]), c, 0, 0, 0);
       } else {
-        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tile.k[h][i].x), __uint_as_float(q[i].x), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tile.k[h][i].y), __uint_as_float(q[i].y), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tile.k[h][i].z), __uint_as_float(q[i].z), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tile.k[h][i].w), __uint_as_float(q[i].w), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k.x), __uint_as_float(q[i].x), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k.y), __uint_as_float(q[i].y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k.z), __uint_as_float(q[i].z), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k.w), __uint_as_float(q[i].w), c, 0, 0, 0);
       }
     }
 #pragma unroll
@@ -104,7 +127,7 @@ __device__ __forceinline__ void pa_accumulate(PaState<T, HD> &st, PaTile<T, HD> 
     for (int h = 0; h < G::NH; ++h)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool dead = !((tile.live >> (h * 16 + g * 4 + i)) & 1u);
+        const bool dead = !((tile.live >> (g * G::NK + h * 4 + i)) & 1u);
         if (dead) s[h][i] = -INFINITY;
         // a weight of zero does not silence a NaN or an infinity: the row itself becomes zero
 #pragma unroll
@@ -169,7 +192,7 @@ __device__ __forceinline__ void pa_accumulate(PaState<T, HD> &st, PaTile<T, HD> 
 // Tiles t0 + wave, t0 + wave + WAVES, .. < t1 of sequence b, K/V head h, query heads h0 .. h0 + gq - 1.  While a tile is
 // worked on the next one of the wave is on its way, and the page numbers of the one behind that.
 template <typename T, int HD, int WAVES>
-__device__ __forceinline__ void pa_run(const PageAttnArgs &a, int b, int len, int h, int h0, int gq, int t0, int t1, PaState<T, HD> &st) {
+__device__ __forceinline__ void pa_run(const PageAttnArgs &a, int b, int len, int h, int h0, int gq, int t0, int t1, char *lds, PaState<T, HD> &st) {
   using G = PaGeo<T, HD>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   st.m = -INFINITY;
@@ -187,25 +210,21 @@ __device__ __forceinline__ void pa_run(const PageAttnArgs &a, int b, int len, in
     if (key < len) pg = row[key >> a.lg];
     return (unsigned)pg < (unsigned)a.n_pages ? pg : -1;
   };
-  const char *kh = a.K + (int64_t)h * a.k_head + g * 16, *vh = a.V + (int64_t)h * a.v_head + m * (G::VW * 4);
+  // K: the lanes of a row side by side, KI tokens one behind the other for each; V: 16 lanes a row, NK tokens.  Either number
+  // divides the smallest page, so the tokens of a lane share one.
+  const int kr = lane / G::C;
+  const char *kh = a.K + (int64_t)h * a.k_head + (lane % G::C) * 16, *vh = a.V + (int64_t)h * a.v_head + m * (G::VW * 4);
   // rows that do not count are read from page 0 (any row of the pool will do) and masked
   auto load = [&](PaTile<T, HD> &d, int tile, int pg) {
     d.live = (uint32_t)__ballot(pg >= 0) & (G::TILE == 32 ? 0xffffffffu : 0xffffu);
     const int key0 = tile * G::TILE, safe = pg < 0 ? 0 : pg;
+    const int kp = __shfl(safe, kr * G::KI, 64), vp = __shfl(safe, g * G::NK, 64);
+    const char *p = kh + (int64_t)kp * a.k_page + (int64_t)((key0 + kr * G::KI) & in_page) * a.k_tok;
 #pragma unroll
-    for (int hh = 0; hh < G::NH; ++hh) {
-      const int page = __shfl(safe, hh * 16 + m, 64);
-      const char *p = kh + (int64_t)page * a.k_page + (int64_t)((key0 + hh * 16 + m) & in_page) * a.k_tok;
+    for (int i = 0; i < G::KI; ++i) d.k[i] = pa_ld16(p + i * a.k_tok);
+    p = vh + (int64_t)vp * a.v_page + (int64_t)((key0 + g * G::NK) & in_page) * a.v_tok;
 #pragma unroll
-      for (int i = 0; i < G::KL; ++i) d.k[hh][i] = ld16(p + i * 64);
-    }
-#pragma unroll
-    for (int hh = 0; hh < G::NH; ++hh) {
-      const int page = __shfl(safe, hh * 16 + g * 4, 64);   // (four tokens from a multiple of four share a page)
-      const char *p = vh + (int64_t)page * a.v_page + (int64_t)((key0 + hh * 16 + g * 4) & in_page) * a.v_tok;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) pa_load_words<G::VW>(d.v[hh * 4 + i], p + i * a.v_tok);
-    }
+    for (int i = 0; i < G::NK; ++i) pa_load_words<G::VW>(d.v[i], p + i * a.v_tok);
   };
   uint4 q[G::KL];
 #pragma unroll
@@ -224,14 +243,14 @@ __device__ __forceinline__ void pa_run(const PageAttnArgs &a, int b, int len, in
       load(y, t + WAVES, next);
       next = pages_of(t + 2 * WAVES < t1 ? t + 2 * WAVES : t);
     }
-    pa_accumulate<T, HD>(st, x, q, a.scale2, g);
+    pa_accumulate<T, HD>(st, x, q, a.scale2, lds);
     t += WAVES;
     if (t >= t1) break;
     if (t + WAVES < t1) {
       load(x, t + WAVES, next);
       next = pages_of(t + 2 * WAVES < t1 ? t + 2 * WAVES : t);
     }
-    pa_accumulate<T, HD>(st, y, q, a.scale2, g);
+    pa_accumulate<T, HD>(st, y, q, a.scale2, lds);
     t += WAVES;
     if (t >= t1) break;
   }
@@ -248,25 +267,29 @@ __device__ __forceinline__ void pa_finish(const PageAttnArgs &a, int b, int head
   if (d == 0 && a.lse) a.lse[(int64_t)head * a.batch + b] = l == 0.f ? -INFINITY : (m + log2f(l)) * PA_LN2;
 }
 
+// LDS of a wave: K of a tile, later its part of the result, [gq][HD + PA_PAD] sums and [gq] (m, l).
 constexpr int PA_PAD = 4;   // words between the rows of two queries
-template <int HD> __host__ __device__ constexpr size_t pa_join_floats(int waves, int gq) { return (size_t)waves * gq * (HD + PA_PAD + 2); }
+template <typename T, int HD> __host__ __device__ constexpr int pa_wave_bytes(int gq) {
+  return gq * (HD + PA_PAD + 2) * 4 > PaGeo<T, HD>::K_BYTES ? (gq * (HD + PA_PAD + 2) * 4 + 15) / 16 * 16 : PaGeo<T, HD>::K_BYTES;
+}
 
 // The waves' parts joined in LDS; record < 0: the result, otherwise a record of partial sums.
 template <typename T, int HD, int WAVES>
-__device__ __forceinline__ void pa_join(const PageAttnArgs &a, float *lds, PaState<T, HD> &st, int b, int h0, int gq, int record) {
+__device__ __forceinline__ void pa_join(const PageAttnArgs &a, char *lds, int wave_bytes, PaState<T, HD> &st, int b, int h0, int gq, int record) {
   using G = PaGeo<T, HD>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-  float *so = lds, *ss = lds + (size_t)WAVES * gq * (HD + PA_PAD);
+  auto so = [&](int w, int n) { return reinterpret_cast<float *>(lds + w * wave_bytes) + n * (HD + PA_PAD); };
+  auto ss = [&](int w, int n) { return reinterpret_cast<float *>(lds + w * wave_bytes) + gq * (HD + PA_PAD) + n * 2; };
   float l = st.l;
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
   if (m < gq) {
-    float *to = so + (size_t)(wave * gq + m) * (HD + PA_PAD);
+    float *to = so(wave, m);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int t = 0; t < G::VT; ++t) to[(g * 4 + i) * G::VT + t] = st.o[t][i];
-    if (g == 0) { ss[(wave * gq + m) * 2] = st.m; ss[(wave * gq + m) * 2 + 1] = l; }
+    if (g == 0) { ss(wave, m)[0] = st.m; ss(wave, m)[1] = l; }
   }
   __syncthreads();
   const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q;   // of a record
@@ -274,13 +297,13 @@ __device__ __forceinline__ void pa_join(const PageAttnArgs &a, float *lds, PaSta
     const int n = i / HD, d = i % HD;
     float top = -INFINITY, sum = 0.f, o = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ss[(w * gq + n) * 2]);
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ss(w, n)[0]);
     const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const float mw = ss[(w * gq + n) * 2], f = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - ref);
-      sum += f * ss[(w * gq + n) * 2 + 1];
-      o += f * so[(size_t)(w * gq + n) * (HD + PA_PAD) + d];
+      const float mw = ss(w, n)[0], f = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - ref);
+      sum += f * ss(w, n)[1];
+      o += f * so(w, n)[d];
     }
     if (record < 0) {
       pa_finish<T>(a, b, h0 + n, d, top, sum, o);
@@ -301,14 +324,16 @@ __device__ __forceinline__ int pa_len(const PageAttnArgs &a, int b) {
 template <typename T, int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_whole_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
-  extern __shared__ float pa_lds[];
+  extern __shared__ __align__(16) char pa_lds[];
+  const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, wave_bytes = pa_wave_bytes<T, HD>(rows);
+  char *own = pa_lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * wave_bytes;
   const int segs = a.kv_heads * a.q_blocks, b = blockIdx.x / segs, seg = blockIdx.x - b * segs;
   const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
   const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
   const int len = pa_len(a, b);
   PaState<T, HD> st;
-  pa_run<T, HD, WAVES>(a, b, len, h, h0, gq, 0, (len + PaGeo<T, HD>::TILE - 1) / PaGeo<T, HD>::TILE, st);
-  pa_join<T, HD, WAVES>(a, pa_lds, st, b, h0, gq, -1);
+  pa_run<T, HD, WAVES>(a, b, len, h, h0, gq, 0, (len + PaGeo<T, HD>::TILE - 1) / PaGeo<T, HD>::TILE, own, st);
+  pa_join<T, HD, WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, -1);
 }
 
 // Split launches.  All tiles of the call, sequence by sequence and in it head by head, are one line that is cut into pieces of
@@ -368,10 +393,11 @@ __device__ __forceinline__ int pa_sequence(const PageAttnArgs &a, const int *bef
 template <typename T, int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_split_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
-  extern __shared__ float pa_lds[];
+  extern __shared__ __align__(16) char pa_lds[];
   __shared__ int scratch[WAVES];
-  const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, segs = a.kv_heads * a.q_blocks;
-  int *before = reinterpret_cast<int *>(pa_lds + pa_join_floats<HD>(WAVES, rows));
+  const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, segs = a.kv_heads * a.q_blocks, wave_bytes = pa_wave_bytes<T, HD>(rows);
+  char *own = pa_lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * wave_bytes;
+  int *before = reinterpret_cast<int *>(pa_lds + WAVES * wave_bytes);
   const PaCut c = pa_cut(a, PaGeo<T, HD>::TILE, segs, before, scratch);
   int64_t at = (int64_t)blockIdx.x * c.piece;
   const int64_t end = at + c.piece < c.tiles ? at + c.piece : c.tiles;
@@ -386,9 +412,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_split_kernel(PageAttn
     const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
     const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
     PaState<T, HD> st;
-    pa_run<T, HD, WAVES>(a, b, pa_len(a, b), h, h0, gq, t0, t1, st);
+    pa_run<T, HD, WAVES>(a, b, pa_len(a, b), h, h0, gq, t0, t1, own, st);
     const int record = t0 == 0 && t1 == nt ? -1 : 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-    pa_join<T, HD, WAVES>(a, pa_lds, st, b, h0, gq, record);
+    pa_join<T, HD, WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, record);
     at += t1 - t0;
     __syncthreads();
   }
@@ -403,7 +429,7 @@ constexpr int PA_JOIN_THREADS = 256;
 template <typename T, int HD, bool BY_PIECE>
 __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
-  extern __shared__ float pa_lds[];
+  extern __shared__ __align__(16) char pa_lds[];
   __shared__ int scratch[PA_JOIN_THREADS / 64];
   __shared__ float tops[PA_MAX_Q], sums[PA_MAX_Q];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -441,7 +467,7 @@ __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAtt
   if (q0 >= gq) return;
   const int nq = q1 - q0;
   __syncthreads();           // (the list of sequences is overwritten)
-  float *weight = pa_lds;    // [nq][n_rec]
+  float *weight = reinterpret_cast<float *>(pa_lds);    // [nq][n_rec]
   auto record = [&](int r) { return (int64_t)(2 * (w0 + r) + (r == 0 ? 1 : 0)) * rows; };
   for (int n = wave; n < nq; n += PA_JOIN_THREADS / 64) {
     float top = -INFINITY, sum = 0.f;
@@ -462,7 +488,7 @@ __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAtt
   // four elements a thread; where these are fewer than the threads, groups of threads take every n-th record
   constexpr int V = HD / 4;
   const int items = nq * V, groups = items < PA_JOIN_THREADS ? PA_JOIN_THREADS / items : 1;
-  float4 *part_sum = reinterpret_cast<float4 *>(pa_lds + (((size_t)nq * n_rec + 3) & ~(size_t)3));   // [groups][items]
+  float4 *part_sum = reinterpret_cast<float4 *>(weight + (((size_t)nq * n_rec + 3) & ~(size_t)3));   // [groups][items]
   for (int i0 = 0; i0 < items; i0 += PA_JOIN_THREADS) {
     const int grp = groups > 1 ? tid / items : 0, i = groups > 1 ? tid - grp * items : i0 + tid;
     const bool mine = grp < groups && i < items;
@@ -501,14 +527,15 @@ inline size_t pa_part_bytes(const lightkv_pages *p) { return (size_t)2 * PA_WGS 
 template <typename T, int HD>
 static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t stream) {
   const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q;
+  const size_t wave_bytes = pa_wave_bytes<T, HD>(rows);
   const unsigned segs = (unsigned)a.batch * (unsigned)(a.kv_heads * a.q_blocks);
   if (whole) {
-    if (rows <= 8) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), pa_join_floats<HD>(8, rows) * sizeof(float), stream, a);
-    else hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 4>), dim3(segs), dim3(256), pa_join_floats<HD>(4, rows) * sizeof(float), stream, a);
+    if (rows <= 8) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), 8 * wave_bytes, stream, a);
+    else hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 4>), dim3(segs), dim3(256), 4 * wave_bytes, stream, a);
     return hipGetLastError();
   }
   const size_t cut = ((size_t)a.batch + 1) * sizeof(int);
-  hipLaunchKernelGGL((page_attn_split_kernel<T, HD, 4>), dim3(a.n_wgs), dim3(256), pa_join_floats<HD>(4, rows) * sizeof(float) + cut, stream, a);
+  hipLaunchKernelGGL((page_attn_split_kernel<T, HD, 4>), dim3(a.n_wgs), dim3(256), 4 * wave_bytes + cut, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // LDS: the list of sequences, then weights of all records and the sums of the thread groups
