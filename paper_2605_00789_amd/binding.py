@@ -381,6 +381,9 @@ def lightkv_compress_schedule_ratio(stages: StageArray, rho, tiles, grid_h, grid
 
 # ---- paged cache ------------------------------------------------------------------------------------------------------
 PAGED_MAX_BATCH = 4096   # LIGHTKV_PAGED_MAX_BATCH
+# the handle of the current stream: 0.1 us, where making a torch.cuda.Stream for it takes 2.7 of a call's 10
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _PAGE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
@@ -419,33 +422,35 @@ class Pages:
         else:
             c.n_pages, c.page_tokens = int(n_pages), int(page_tokens)
         self._ref = C.byref(c)
+        # what every call looks at, without a trip through ctypes or a torch.device (a call's host time is its cost for few rows)
+        self.index, self.batch, self.heads, self.kv_heads, self.head_dim = self.device.index, c.batch, c.heads, c.kv_heads, c.head_dim
+        self.n_pages = c.n_pages
 
     def _ints(self, t, n, what):
         """An int32 array of at least n entries on the cache's device."""
-        if t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous() or t.numel() < n:
-            raise ValueError("%s: contiguous int32 of at least %d entries on the table's device" % (what, n))
-        return t.data_ptr()
+        if t.dtype is torch.int32 and t.get_device() == self.index and t.numel() >= n and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError("%s: contiguous int32 of at least %d entries on the table's device" % (what, n))
 
     def _rows(self, t, heads, n, what):
         """Rows [n or more, heads, head_dim] (or [.., heads * head_dim]): pointer and strides."""
-        d = self.c.head_dim
-        if t.dtype != self.dtype or t.device != self.device:
+        if t.dtype is not self.dtype or t.get_device() != self.index:
             raise ValueError("%s: %s on the table's device" % (what, self.dtype))
-        if t.dim() == 3 and t.shape[1] == heads and t.shape[2] == d and t.stride(2) == 1 and t.shape[0] >= n:
-            return t.data_ptr(), t.stride(0), t.stride(1)
-        if t.dim() == 2 and t.shape[1] == heads * d and t.stride(1) == 1 and t.shape[0] >= n:
-            return t.data_ptr(), t.stride(0), d
+        shape, stride, d = t.shape, t.stride(), self.head_dim
+        if len(shape) == 3:
+            if shape[1] == heads and shape[2] == d and stride[2] == 1 and shape[0] >= n:
+                return t.data_ptr(), stride[0], stride[1]
+        elif len(shape) == 2 and shape[1] == heads * d and stride[1] == 1 and shape[0] >= n:
+            return t.data_ptr(), stride[0], d
         raise ValueError("%s: [%d or more, %d, %d] with contiguous elements" % (what, n, heads, d))
 
     def _call(self, fn, where, args, stream):
         """The call on its stream: that of the cache's device, with this device current."""
-        if torch.cuda.current_device() == self.device.index:
-            s = torch.cuda.current_stream() if stream is None else stream
-            st = fn(self._ref, *args, s.cuda_stream)
+        if _current_device() == self.index:
+            st = fn(self._ref, *args, _raw_stream(self.index) if stream is None else stream.cuda_stream)
         else:
             with torch.cuda.device(self.device):
-                s = torch.cuda.current_stream() if stream is None else stream
-                st = fn(self._ref, *args, s.cuda_stream)
+                st = fn(self._ref, *args, _raw_stream(self.index) if stream is None else stream.cuda_stream)
         if st != 0:
             raise LightKVError(st, where)
 
@@ -454,8 +459,8 @@ def lightkv_page_alloc(p: Pages, cu_new, seq_lens, free_pages, free_count, seq_l
                        status=None, stream=None):
     """Pages and slots for cu_new[b + 1] - cu_new[b] more tokens of every sequence; seq_lens_out and free_count_out may be
     seq_lens and free_count themselves."""
-    n, ints = p.c.batch, p._ints
-    args = (ints(cu_new, n + 1, "cu_new"), ints(seq_lens, n, "seq_lens"), ints(free_pages, p.c.n_pages, "free_pages"),
+    n, ints = p.batch, p._ints
+    args = (ints(cu_new, n + 1, "cu_new"), ints(seq_lens, n, "seq_lens"), ints(free_pages, p.n_pages, "free_pages"),
             ints(free_count, 1, "free_count"), ints(seq_lens_out, n, "seq_lens_out"),
             ints(free_count_out, 1, "free_count_out"), ints(slots, 0, "slots"), slots.numel(),
             None if status is None else ints(status, n, "status"))
@@ -464,8 +469,8 @@ def lightkv_page_alloc(p: Pages, cu_new, seq_lens, free_pages, free_count, seq_l
 
 def lightkv_page_free(p: Pages, done, seq_lens, free_pages, free_count, seq_lens_out, free_count_out, *, stream=None):
     """Pages of every sequence with done[b] != 0 back onto the stack."""
-    n, ints = p.c.batch, p._ints
-    args = (ints(done, n, "done"), ints(seq_lens, n, "seq_lens"), ints(free_pages, p.c.n_pages, "free_pages"),
+    n, ints = p.batch, p._ints
+    args = (ints(done, n, "done"), ints(seq_lens, n, "seq_lens"), ints(free_pages, p.n_pages, "free_pages"),
             ints(free_count, 1, "free_count"), ints(seq_lens_out, n, "seq_lens_out"),
             ints(free_count_out, 1, "free_count_out"))
     p._call(_lib.lightkv_page_free, "lightkv_page_free", args, stream)
@@ -477,10 +482,10 @@ def lightkv_page_write(p: Pages, slots, K, V, *, cu_new=None, stream=None):
     rows = min(t.shape[0] for t in (K, V, slots) if t is not None)
     if rows == 0:
         return
-    h = p.c.kv_heads
+    h = p.kv_heads
     k = (None, 0, 0) if K is None else p._rows(K, h, rows, "K")
     v = (None, 0, 0) if V is None else p._rows(V, h, rows, "V")
-    args = (None if cu_new is None else p._ints(cu_new, p.c.batch + 1, "cu_new"), p._ints(slots, rows, "slots"), rows, *k, *v)
+    args = (None if cu_new is None else p._ints(cu_new, p.batch + 1, "cu_new"), p._ints(slots, rows, "slots"), rows, *k, *v)
     p._call(_lib.lightkv_page_write, "lightkv_page_write", args, stream)
 
 
@@ -493,12 +498,12 @@ def lightkv_page_attention_workspace(p: Pages) -> int:
 def lightkv_page_attention(p: Pages, seq_lens, Q, out, ws, *, lse=None, softmax_scale=0.0, max_seq_tokens=0, stream=None):
     """Attention of one new token per sequence: Q, out [batch, heads, head_dim] (or [batch, heads * head_dim]); lse: optional
     fp32 [heads, batch]; ws: uint8 of lightkv_page_attention_workspace(p) bytes."""
-    c = p.c
-    if lse is not None and (lse.dtype != torch.float32 or lse.device != p.device or not lse.is_contiguous() or lse.numel() < c.heads * c.batch):
+    n, heads = p.batch, p.heads
+    if lse is not None and (lse.dtype is not torch.float32 or lse.get_device() != p.index or lse.numel() < heads * n or not lse.is_contiguous()):
         raise ValueError("lse: contiguous float32 [heads, batch] on the table's device")
-    if ws.device != p.device:
-        raise ValueError("ws on the table's device")
-    args = (p._ints(seq_lens, c.batch, "seq_lens"), int(max_seq_tokens), *p._rows(Q, c.heads, c.batch, "Q"), float(softmax_scale),
-            *p._rows(out, c.heads, c.batch, "out"), None if lse is None else lse.data_ptr(), ws.data_ptr(),
-            ws.numel() * ws.element_size())
+    if ws.get_device() != p.index or not ws.is_contiguous():
+        raise ValueError("ws: contiguous memory on the table's device")
+    args = (p._ints(seq_lens, n, "seq_lens"), int(max_seq_tokens), *p._rows(Q, heads, n, "Q"), float(softmax_scale),
+            *p._rows(out, heads, n, "out"), None if lse is None else lse.data_ptr(), ws.data_ptr(),
+            ws.nbytes)
     p._call(_lib.lightkv_page_attention, "lightkv_page_attention", args, stream)
