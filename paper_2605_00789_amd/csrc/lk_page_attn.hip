@@ -28,6 +28,7 @@ struct PageAttnArgs {
   const char *K, *V, *Q;
   char *out;
   float *lse, *stats, *part;      // records of partial results: (m, l) and unscaled sums
+  int4 *cuts;                     // (sequence, segment, first piece, records) of what the second launch joins
   const int32_t *table, *seq_lens;
   int64_t table_stride;
   int64_t k_page, k_tok, k_head, v_page, v_tok, v_head, q_tok, q_head, o_tok, o_head;   // bytes
@@ -342,6 +343,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_whole_kernel(PageAttn
 // parts become records 2 w and 2 w + 1, which the second kernel joins.
 struct PaCut { int total; int64_t tiles, piece; };
 
+// Quotient of numbers that are small in all but impossible calls: a 64-bit division is 130 instructions.
+__device__ __forceinline__ int64_t pa_quotient(int64_t n, int64_t d) {
+  return ((n | d) >> 32) == 0 ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
+}
+
 // before[b] = tiles of one head in the sequences before b; the whole workgroup.
 __device__ __forceinline__ PaCut pa_cut(const PageAttnArgs &a, int tile, int segs, int *before, int *scratch) {
   const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, wave = tid >> 6;
@@ -374,7 +380,7 @@ __device__ __forceinline__ PaCut pa_cut(const PageAttnArgs &a, int tile, int seg
   PaCut c;
   c.total = total;
   c.tiles = (int64_t)total * segs;
-  c.piece = (c.tiles + a.n_wgs - 1) / a.n_wgs;
+  c.piece = pa_quotient(c.tiles + a.n_wgs - 1, a.n_wgs);
   c.piece = c.piece < a.min_tiles ? a.min_tiles : c.piece;
   return c;
 }
@@ -390,104 +396,128 @@ __device__ __forceinline__ int pa_sequence(const PageAttnArgs &a, const int *bef
   return lo;
 }
 
-template <typename T, int HD, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void page_attn_split_kernel(PageAttnArgs a) {
+constexpr int PA_WGS = 512;          // workgroups of a split launch: two of four waves fit a CU
+constexpr int PA_SPLIT_WAVES = 4, PA_JOIN_THREADS = 256;
+
+// A segment that is cut belongs to the piece in which it begins: cuts[piece], at most one per piece, tells the second launch
+// about it.  Where the call has fewer segments than pieces the entries are those of the segments instead (BY_PIECE false).
+template <typename T, int HD, bool BY_PIECE>
+__global__ __launch_bounds__(PA_SPLIT_WAVES * 64, 2) void page_attn_split_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
   extern __shared__ __align__(16) char pa_lds[];
-  __shared__ int scratch[WAVES];
+  __shared__ int scratch[PA_SPLIT_WAVES];
   const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, segs = a.kv_heads * a.q_blocks, wave_bytes = pa_wave_bytes<T, HD>(rows);
   char *own = pa_lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * wave_bytes;
-  int *before = reinterpret_cast<int *>(pa_lds + WAVES * wave_bytes);
+  int *before = reinterpret_cast<int *>(pa_lds + PA_SPLIT_WAVES * wave_bytes);
   const PaCut c = pa_cut(a, PaGeo<T, HD>::TILE, segs, before, scratch);
+  for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {   // sequences without tokens
+    if (before[b + 1] != before[b]) continue;
+    for (int i = threadIdx.x; i < a.kv_heads * a.group * HD; i += PA_SPLIT_WAVES * 64) pa_finish<T>(a, b, i / HD, i % HD, 0.f, 0.f, 0.f);
+    if (!BY_PIECE)
+      for (int i = threadIdx.x; i < segs; i += PA_SPLIT_WAVES * 64) a.cuts[b * segs + i] = int4{0, 0, 0, 0};
+  }
   int64_t at = (int64_t)blockIdx.x * c.piece;
   const int64_t end = at + c.piece < c.tiles ? at + c.piece : c.tiles;
-  if (at >= end) return;
-  int b = pa_sequence(a, before, segs, at);
-  while (at < end) {
-    while ((int64_t)before[b + 1] * segs <= at) ++b;   // (ends: at < tiles)
-    const int nt = before[b + 1] - before[b];
-    const int64_t local = at - (int64_t)before[b] * segs;
-    const int seg = (int)(local / nt), t0 = (int)(local - (int64_t)seg * nt);
-    const int t1 = end - at < nt - t0 ? t0 + (int)(end - at) : nt;
-    const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
-    const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
-    PaState<T, HD> st;
-    pa_run<T, HD, WAVES>(a, b, pa_len(a, b), h, h0, gq, t0, t1, own, st);
-    const int record = t0 == 0 && t1 == nt ? -1 : 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-    pa_join<T, HD, WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, record);
-    at += t1 - t0;
-    __syncthreads();
+  int4 cut = {0, 0, 0, 0};
+  if (at < end) {
+    int b = pa_sequence(a, before, segs, at);
+    while (at < end) {
+      while ((int64_t)before[b + 1] * segs <= at) ++b;   // (ends: at < tiles)
+      const int nt = before[b + 1] - before[b];
+      const int64_t local = at - (int64_t)before[b] * segs;
+      const int seg = (int)pa_quotient(local, nt), t0 = (int)(local - (int64_t)seg * nt);
+      const int t1 = end - at < nt - t0 ? t0 + (int)(end - at) : nt;
+      const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
+      const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
+      PaState<T, HD> st;
+      pa_run<T, HD, PA_SPLIT_WAVES>(a, b, pa_len(a, b), h, h0, gq, t0, t1, own, st);
+      const int record = t0 == 0 && t1 == nt ? -1 : 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
+      pa_join<T, HD, PA_SPLIT_WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, record);
+      if (t0 == 0) {
+        const int4 mine = {b, seg, (int)blockIdx.x, (int)pa_quotient(at + nt - 1, c.piece) - (int)blockIdx.x + 1};
+        if (t1 < nt) cut = mine;
+        if (!BY_PIECE && threadIdx.x == 0) a.cuts[b * segs + seg] = mine;
+      }
+      at += t1 - t0;
+      __syncthreads();
+    }
   }
+  if (BY_PIECE && threadIdx.x == 0) a.cuts[blockIdx.x] = cut;
 }
 
-constexpr int PA_WGS = 512;          // workgroups of a split launch: two of four waves fit a CU
-constexpr int PA_JOIN_THREADS = 256;
+// Joins the records of a segment: one workgroup per piece that a cut segment begins in, or per segment and query head where
+// segments are few and their records many.  The beginning of a segment is its piece's second record, the rest are first
+// records, and they are added in this order.
+constexpr int PA_FEW = 4;   // records that a thread loads at once, weights and sums, in one trip to memory
 
-// Joins the records of a segment, and writes what sequences without tokens get.  A segment that is cut belongs to the
-// workgroup of the split launch in which it begins, so there are at most n_wgs of them: BY_PIECE takes one per workgroup.
-// With fewer segments than that a workgroup takes a segment (and one query head of it, blockIdx.y, as records are many then).
 template <typename T, int HD, bool BY_PIECE>
 __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
   extern __shared__ __align__(16) char pa_lds[];
-  __shared__ int scratch[PA_JOIN_THREADS / 64];
   __shared__ float tops[PA_MAX_Q], sums[PA_MAX_Q];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, segs = a.kv_heads * a.q_blocks;
-  int *before = reinterpret_cast<int *>(pa_lds);
-  const PaCut c = pa_cut(a, PaGeo<T, HD>::TILE, segs, before, scratch);
-  for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
-    if (before[b + 1] != before[b] || blockIdx.y) continue;
-    for (int i = tid; i < a.kv_heads * a.group * HD; i += PA_JOIN_THREADS) pa_finish<T>(a, b, i / HD, i % HD, 0.f, 0.f, 0.f);
-  }
-  int b, seg, nt, w0;
-  int64_t first;
-  if (BY_PIECE) {
-    w0 = blockIdx.x;
-    const int64_t end = (int64_t)(w0 + 1) * c.piece;
-    if (end >= c.tiles) return;
-    b = pa_sequence(a, before, segs, end);
-    nt = before[b + 1] - before[b];
-    const int64_t local = end - (int64_t)before[b] * segs;
-    seg = (int)(local / nt);
-    first = (int64_t)before[b] * segs + (int64_t)seg * nt;
-    if (first == end || first < end - c.piece) return;   // cut in front of a segment; one that began earlier
-  } else {
-    b = blockIdx.x / segs; seg = blockIdx.x - b * segs;
-    nt = before[b + 1] - before[b];
-    if (nt == 0) return;
-    first = (int64_t)before[b] * segs + (int64_t)seg * nt;
-    w0 = (int)(first / c.piece);
-  }
-  const int n_rec = (int)((first + nt - 1) / c.piece) - w0 + 1;
-  if (n_rec == 1) return;    // one workgroup had it all
+  const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q;
+  const int4 cut = a.cuts[blockIdx.x];
+  const int b = cut.x, seg = cut.y, w0 = cut.z, n_rec = cut.w;
+  if (n_rec <= 1) return;    // no segment, or one workgroup had it all
   const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
   const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
-  const int q0 = BY_PIECE ? 0 : blockIdx.y, q1 = BY_PIECE ? gq : q0 + 1;
+  const int q0 = BY_PIECE ? 0 : blockIdx.y, nq = BY_PIECE ? gq : 1;
   if (q0 >= gq) return;
-  const int nq = q1 - q0;
-  __syncthreads();           // (the list of sequences is overwritten)
+  constexpr int V = HD / 4;   // four elements a thread
+  const int items = nq * V;
+  auto record = [&](int r) { return (int64_t)(2 * (w0 + r) + (r == 0 ? 1 : 0)) * rows + q0; };
+  auto finish = [&](int n, int d, float top, float sum, const float4 &o) {
+    const float e[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) pa_finish<T>(a, b, h0 + q0 + n, d + k, top, sum, e[k]);
+  };
+  if (n_rec <= PA_FEW) {
+    for (int i = tid; i < items; i += PA_JOIN_THREADS) {
+      const int n = i / V, d = (i - n * V) * 4;
+      float2 s[PA_FEW];
+      float4 v[PA_FEW];
+#pragma unroll
+      for (int r = 0; r < PA_FEW; ++r) {
+        const int64_t k = record(r < n_rec ? r : 0) + n;
+        s[r] = *reinterpret_cast<const float2 *>(a.stats + k * 2);
+        v[r] = *reinterpret_cast<const float4 *>(a.part + k * HD + d);
+      }
+      float top = s[0].x, sum = 0.f;
+#pragma unroll
+      for (int r = 1; r < PA_FEW; ++r) top = fmaxf(top, s[r].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < PA_FEW; ++r) {
+        if (r >= n_rec) continue;
+        const float f = s[r].x == top ? 1.f : __builtin_amdgcn_exp2f(s[r].x - ref);
+        sum += f * s[r].y;
+        o.x += f * v[r].x; o.y += f * v[r].y; o.z += f * v[r].z; o.w += f * v[r].w;
+      }
+      finish(n, d, top, sum, o);
+    }
+    return;
+  }
   float *weight = reinterpret_cast<float *>(pa_lds);    // [nq][n_rec]
-  auto record = [&](int r) { return (int64_t)(2 * (w0 + r) + (r == 0 ? 1 : 0)) * rows; };
   for (int n = wave; n < nq; n += PA_JOIN_THREADS / 64) {
     float top = -INFINITY, sum = 0.f;
-    for (int r = lane; r < n_rec; r += 64) top = fmaxf(top, a.stats[(record(r) + q0 + n) * 2]);
+    for (int r = lane; r < n_rec; r += 64) top = fmaxf(top, a.stats[(record(r) + n) * 2]);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     const float ref = top == -INFINITY ? 0.f : top;
     for (int r = lane; r < n_rec; r += 64) {
-      const float *s = a.stats + (record(r) + q0 + n) * 2;
-      const float f = s[0] == top ? 1.f : __builtin_amdgcn_exp2f(s[0] - ref);
+      const float2 s = *reinterpret_cast<const float2 *>(a.stats + (record(r) + n) * 2);
+      const float f = s.x == top ? 1.f : __builtin_amdgcn_exp2f(s.x - ref);
       weight[n * n_rec + r] = f;
-      sum += f * s[1];
+      sum += f * s.y;
     }
     sum = wave_sum_butterfly(sum);
     if (lane == 0) { tops[n] = top; sums[n] = sum; }
   }
   __syncthreads();
-  // four elements a thread; where these are fewer than the threads, groups of threads take every n-th record
-  constexpr int V = HD / 4;
-  const int items = nq * V, groups = items < PA_JOIN_THREADS ? PA_JOIN_THREADS / items : 1;
+  // where the items are fewer than the threads, groups of threads take every n-th record
+  const int groups = items < PA_JOIN_THREADS ? PA_JOIN_THREADS / items : 1;
   float4 *part_sum = reinterpret_cast<float4 *>(weight + (((size_t)nq * n_rec + 3) & ~(size_t)3));   // [groups][items]
   for (int i0 = 0; i0 < items; i0 += PA_JOIN_THREADS) {
     const int grp = groups > 1 ? tid / items : 0, i = groups > 1 ? tid - grp * items : i0 + tid;
@@ -497,7 +527,7 @@ __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAtt
     if (mine) {
 #pragma unroll 8
       for (int r = grp; r < n_rec; r += groups) {
-        const float4 v = *reinterpret_cast<const float4 *>(a.part + (record(r) + q0 + n) * HD + d);
+        const float4 v = *reinterpret_cast<const float4 *>(a.part + (record(r) + n) * HD + d);
         const float f = weight[n * n_rec + r];
         o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
       }
@@ -511,18 +541,17 @@ __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAtt
         o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
       }
     }
-    if (!mine) continue;
-    const float e[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) pa_finish<T>(a, b, h0 + q0 + n, d + k, tops[n], sums[n], e[k]);
+    if (mine) finish(n, d, tops[n], sums[n], o);
   }
 }
 
 constexpr int PA_WHOLE_TOKENS = 1024;
+constexpr unsigned PA_WIDE_SEGS = 256;
 
 inline int pa_rows(const lightkv_pages *p) { const int g = p->heads / p->kv_heads; return g < PA_MAX_Q ? g : PA_MAX_Q; }
 inline size_t pa_stat_bytes(const lightkv_pages *p) { return ((size_t)2 * PA_WGS * pa_rows(p) * 2 * sizeof(float) + 255) / 256 * 256; }
 inline size_t pa_part_bytes(const lightkv_pages *p) { return (size_t)2 * PA_WGS * pa_rows(p) * p->head_dim * sizeof(float); }
+inline size_t pa_bytes(const lightkv_pages *p) { return pa_stat_bytes(p) + pa_part_bytes(p) + PA_WGS * sizeof(int4); }
 
 template <typename T, int HD>
 static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t stream) {
@@ -530,19 +559,22 @@ static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t strea
   const size_t wave_bytes = pa_wave_bytes<T, HD>(rows);
   const unsigned segs = (unsigned)a.batch * (unsigned)(a.kv_heads * a.q_blocks);
   if (whole) {
-    if (rows <= 8) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), 8 * wave_bytes, stream, a);
+    if (rows <= 8 && segs <= PA_WIDE_SEGS) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), 8 * wave_bytes, stream, a);
     else hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 4>), dim3(segs), dim3(256), 4 * wave_bytes, stream, a);
     return hipGetLastError();
   }
-  const size_t cut = ((size_t)a.batch + 1) * sizeof(int);
-  hipLaunchKernelGGL((page_attn_split_kernel<T, HD, 4>), dim3(a.n_wgs), dim3(256), 4 * wave_bytes + cut, stream, a);
+  const size_t list = ((size_t)a.batch + 1) * sizeof(int);   // of the sequences, behind the waves' LDS
+  const dim3 wgs(a.n_wgs), threads(PA_SPLIT_WAVES * 64);
+  const bool by_piece = segs >= (unsigned)a.n_wgs;
+  // records of a segment: all segments of a sequence are equally long, so n_wgs / (their number) + 2 at most
+  const size_t most = a.n_wgs / (size_t)(a.kv_heads * a.q_blocks) + 2;
+  const size_t join = (((by_piece ? rows : 1) * most + 3) / 4 * 4 + 4 * PA_JOIN_THREADS) * sizeof(float);
+  if (by_piece) hipLaunchKernelGGL((page_attn_split_kernel<T, HD, true>), wgs, threads, PA_SPLIT_WAVES * wave_bytes + list, stream, a);
+  else hipLaunchKernelGGL((page_attn_split_kernel<T, HD, false>), wgs, threads, PA_SPLIT_WAVES * wave_bytes + list, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // LDS: the list of sequences, then weights of all records and the sums of the thread groups
-  const bool by_piece = segs >= (unsigned)a.n_wgs;
-  const size_t join = ((size_t)(by_piece ? rows : 1) * (a.n_wgs + 1) + 4) * sizeof(float) + (size_t)PA_JOIN_THREADS * sizeof(float4), lds = join > cut ? join : cut;
-  if (by_piece) hipLaunchKernelGGL((page_attn_join_kernel<T, HD, true>), dim3(a.n_wgs), dim3(PA_JOIN_THREADS), lds, stream, a);
-  else hipLaunchKernelGGL((page_attn_join_kernel<T, HD, false>), dim3(segs, rows), dim3(PA_JOIN_THREADS), lds, stream, a);
+  if (by_piece) hipLaunchKernelGGL((page_attn_join_kernel<T, HD, true>), wgs, dim3(PA_JOIN_THREADS), join, stream, a);
+  else hipLaunchKernelGGL((page_attn_join_kernel<T, HD, false>), dim3(segs, rows), dim3(PA_JOIN_THREADS), join, stream, a);
   return hipGetLastError();
 }
 
@@ -566,7 +598,7 @@ extern "C" {
 lightkv_status lightkv_page_attention_workspace(const lightkv_pages *p, size_t *bytes) {
   if (!bytes) return LIGHTKV_ERR_NULL;
   const lightkv_status st = check_page_attention(p);
-  if (st == LIGHTKV_OK) *bytes = pa_stat_bytes(p) + pa_part_bytes(p);
+  if (st == LIGHTKV_OK) *bytes = pa_bytes(p);
   return st;
 }
 
@@ -593,11 +625,12 @@ lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq
   if (p->heads > 1 && o_head_stride < p->head_dim) return LIGHTKV_ERR_SHAPE;
   if (p->batch > 1 && o_tok_stride < p->head_dim) return LIGHTKV_ERR_SHAPE;
   const size_t stat = pa_stat_bytes(p);
-  if (!ws || !aligned_to(ws, 256) || ws_bytes < stat + pa_part_bytes(p)) return LIGHTKV_ERR_WORKSPACE;
+  if (!ws || !aligned_to(ws, 256) || ws_bytes < pa_bytes(p)) return LIGHTKV_ERR_WORKSPACE;
   PageAttnArgs a{};
   a.K = static_cast<const char *>(p->K); a.V = static_cast<const char *>(p->V);
   a.Q = static_cast<const char *>(Q); a.out = static_cast<char *>(out); a.lse = lse;
   a.stats = static_cast<float *>(ws); a.part = reinterpret_cast<float *>(static_cast<char *>(ws) + stat);
+  a.cuts = reinterpret_cast<int4 *>(static_cast<char *>(ws) + stat + pa_part_bytes(p));
   a.table = p->table; a.seq_lens = seq_lens; a.table_stride = p->table_stride;
   // an axis of one entry has no stride
   a.k_page = p->n_pages > 1 ? p->k_page_stride * eb : 0; a.k_tok = p->k_tok_stride * eb; a.k_head = p->kv_heads > 1 ? p->k_head_stride * eb : 0;
