@@ -28,13 +28,13 @@ struct PageAttnArgs {
   const char *K, *V, *Q;
   char *out;
   float *lse, *stats, *part;      // records of partial results: (m, l) and unscaled sums
-  int4 *cuts;                     // (sequence, segment, first piece, records) of what the second launch joins
+  int4 *cuts;                     // how many cut segments there are; (sequence, segment, first record, records) of each
   const int32_t *table, *seq_lens;
   int64_t table_stride;
   int64_t k_page, k_tok, k_head, v_page, v_tok, v_head, q_tok, q_head, o_tok, o_head;   // bytes
   int batch, kv_heads, group, q_blocks;   // query heads per K/V head, blocks of at most 16 of them
   int n_pages, lg, room;          // room: tokens a table row can hold
-  int n_wgs, min_tiles;           // split launches: workgroups, and the fewest tiles one takes
+  int min_tiles;                  // split launches: a part has as many tiles, if its segment has
   float scale2;                   // softmax scale * log2(e)
 };
 
@@ -337,136 +337,196 @@ __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_whole_kernel(PageAttn
   pa_join<T, HD, WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, -1);
 }
 
-// Split launches.  All tiles of the call, sequence by sequence and in it head by head, are one line that is cut into pieces of
-// equal length, a workgroup each: the cut goes by what there is to do, whatever the lengths are, and needs nothing from the host.
-// A piece covers the end of a segment, whole segments, and the beginning of another: whole ones are finished at once, the two
-// parts become records 2 w and 2 w + 1, which the second kernel joins.
-struct PaCut { int total; int64_t tiles, piece; };
+// Split launches.  A segment (a sequence's K/V head and block of query heads) is cut into parts of at most c tiles, a
+// workgroup each, with c chosen from the lengths on the device so that there are about PA_PARTS parts in all: the cut goes by
+// what there is to do and needs nothing from the host.  More parts than fit the card at once, so that some begin (a chain of
+// loads: lengths, page numbers, rows) while others are in the middle of theirs.  Parts of a segment that is not whole leave
+// records, in the order of their tokens, which a second launch joins.
+constexpr int PA_SPLIT_WAVES = 4, PA_JOIN_THREADS = 256;
+constexpr int PA_PARTS = 1024, PA_SLOTS = 512, PA_FEW_SEGS = 192;
 
 // Quotient of numbers that are small in all but impossible calls: a 64-bit division is 130 instructions.
 __device__ __forceinline__ int64_t pa_quotient(int64_t n, int64_t d) {
   return ((n | d) >> 32) == 0 ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
 }
 
-// before[b] = tiles of one head in the sequences before b; the whole workgroup.
-__device__ __forceinline__ PaCut pa_cut(const PageAttnArgs &a, int tile, int segs, int *before, int *scratch) {
-  const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (a.batch + threads - 1) / threads, b0 = tid * per, b1 = b0 + per < a.batch ? b0 + per : a.batch;
-  int mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    before[b] = (pa_len(a, b) + tile - 1) / tile;
-    mine += before[b];
-  }
-  int incl = mine;
+// Inclusive running sum over the wave.
+__device__ __forceinline__ int wave_running_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8: inside rows of 16 lanes
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // lane 15 of a row to the next row: rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2 and 3
+  return v;
+}
+
+__device__ __forceinline__ int wave_running_max(int v) {   // of numbers that are not negative
+  auto larger = [](int x, int y) { return x > y ? x : y; };
+  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+  return v;
+}
+
+// What a workgroup of a split launch has to do: part `part` of `parts` of segment `seg` of sequence b.
+struct PaPart { int b, len, seg, part, parts, record, cut; };
+
+struct PaCutLds { int sums[2][PA_SPLIT_WAVES], used[PA_SPLIT_WAVES], longest[PA_SPLIT_WAVES], parts[PA_SPLIT_WAVES], records[PA_SPLIT_WAVES], cuts[PA_SPLIT_WAVES]; PaPart mine; };
+
+// Finds part `which` of the call (false: there are fewer).  Every thread takes a run of sequences; the one that owns the part
+// says so.  Parts of cut segments come first, whole segments, which are no longer than those, fill in behind them.
+// all_cuts: cut segments of the call.
+template <int TILE>
+__device__ __forceinline__ bool pa_find_part(const PageAttnArgs &a, int segs, int64_t which, PaCutLds &lds, PaPart &out, int &all_cuts) {
+  constexpr int THREADS = PA_SPLIT_WAVES * 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (a.batch + THREADS - 1) / THREADS, b0 = tid * per, b1 = b0 + per < a.batch ? b0 + per : a.batch;
+  auto sum_of_all = [&](int v, int *scratch) {
+    const int s = wave_running_sum(v);
+    if (lane == 63) scratch[wave] = s;
+    __syncthreads();
+    int all = 0;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += u;
-  }
-  if (lane == 63) scratch[wave] = incl;
-  __syncthreads();
-  int at = incl - mine, total = 0;
-  for (int w = 0; w < threads / 64; ++w) {
-    if (w < wave) at += scratch[w];
-    total += scratch[w];
-  }
+    for (int w = 0; w < PA_SPLIT_WAVES; ++w) all += scratch[w];
+    return all;
+  };
+  auto tiles_of = [&](int len) { return (uint32_t)(len + TILE - 1) / TILE; };
+  // a sequence without tokens is one part, too: it writes what such a sequence gets
+  auto parts_of = [&](int len, uint32_t c) { const uint32_t nt = tiles_of(len); return nt <= c ? 1 : (int)((nt + c - 1) / c); };
+  if (tid == 0) lds.mine.b = -1;
+  int tiles = 0, used = 0, longest = 0;
   for (int b = b0; b < b1; ++b) {
-    const int n = before[b];
-    before[b] = at;
-    at += n;
+    const int n = (int)tiles_of(pa_len(a, b));
+    tiles += n;
+    used += n > 0;
+    longest = n > longest ? n : longest;
   }
-  if (tid == 0) before[a.batch] = total;
+  const int wave_tiles = wave_running_sum(tiles), wave_used = wave_running_sum(used), wave_longest = wave_running_max(longest);
+  if (lane == 63) { lds.sums[0][wave] = wave_tiles; lds.used[wave] = wave_used; lds.longest[wave] = wave_longest; }
   __syncthreads();
-  PaCut c;
-  c.total = total;
-  c.tiles = (int64_t)total * segs;
-  c.piece = pa_quotient(c.tiles + a.n_wgs - 1, a.n_wgs);
-  c.piece = c.piece < a.min_tiles ? a.min_tiles : c.piece;
-  return c;
-}
-
-// The sequence that tile `at` of the line lies in (at < all tiles).
-__device__ __forceinline__ int pa_sequence(const PageAttnArgs &a, const int *before, int segs, int64_t at) {
-  int lo = 0, hi = a.batch;    // last sequence that begins at or before it: one with tiles, since empty ones begin where the next does
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if ((int64_t)before[mid] * segs <= at) lo = mid;
-    else hi = mid;
+  tiles = used = longest = 0;
+#pragma unroll
+  for (int w = 0; w < PA_SPLIT_WAVES; ++w) {
+    tiles += lds.sums[0][w];
+    used += lds.used[w];
+    longest = lds.longest[w] > longest ? lds.longest[w] : longest;
   }
-  return lo;
+  const int64_t n_segs = (int64_t)used * segs, all_tiles = (int64_t)tiles * segs;
+  const bool alike = (int64_t)longest * used * 2 <= (int64_t)tiles * 3;
+  uint32_t c;
+  if (alike) {
+    // k parts of each segment fit the card at once
+    const uint32_t k = n_segs < PA_SLOTS ? PA_SLOTS / (uint32_t)(n_segs ? n_segs : 1) : 1;
+    c = ((uint32_t)longest + k - 1) / k;
+    c = c < (uint32_t)a.min_tiles ? a.min_tiles : c;
+  } else {
+    const int target = n_segs < PA_FEW_SEGS ? PA_SLOTS : PA_PARTS;
+    const int64_t want = pa_quotient(all_tiles + target - 1, target);
+    c = want < a.min_tiles ? a.min_tiles : (uint32_t)want;
+    // rounded up segment by segment they are more than that: longer ones, then
+    int n = 0;
+    for (int b = b0; b < b1; ++b) n += parts_of(pa_len(a, b), c);
+    int64_t all = (int64_t)sum_of_all(n, lds.sums[1]) * segs;
+    all = all < 2 * target ? all : 2 * target;
+    if (all > target) c = (uint32_t)pa_quotient((int64_t)c * all + target - 1, target);
+  }
+  int parts = 0;
+  int records = 0, cuts = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int n = parts_of(pa_len(a, b), c);
+    if (n > 1) { records += n; ++cuts; }
+    else ++parts;
+  }
+  const int sum_parts = wave_running_sum(parts), sum_records = wave_running_sum(records), sum_cuts = wave_running_sum(cuts);
+  if (lane == 63) { lds.parts[wave] = sum_parts; lds.records[wave] = sum_records; lds.cuts[wave] = sum_cuts; }
+  __syncthreads();
+  int at = sum_parts - parts, rec = sum_records - records, cut = sum_cuts - cuts, all_records = 0;
+  all_cuts = 0;
+#pragma unroll
+  for (int w = 0; w < PA_SPLIT_WAVES; ++w) {
+    if (w < wave) { at += lds.parts[w]; rec += lds.records[w]; cut += lds.cuts[w]; }
+    all_cuts += lds.cuts[w];
+    all_records += lds.records[w];
+  }
+  all_cuts *= segs;
+  const bool whole = which >= (int64_t)all_records * segs;
+  const int64_t place = whole ? which - (int64_t)all_records * segs : which;   // among its kind
+  const int mine = whole ? at : rec, count = whole ? parts : records;
+  if (place >= (int64_t)mine * segs && place < (int64_t)(mine + count) * segs) {
+    for (int b = b0; b < b1; ++b) {
+      const int len = pa_len(a, b), n = parts_of(len, c);
+      if ((n == 1) != whole) continue;
+      const int before = whole ? at : rec;
+      if (place < (int64_t)(before + n) * segs) {
+        const uint32_t local = (uint32_t)(place - (int64_t)before * segs), seg = n == 1 ? local : local / (uint32_t)n;
+        lds.mine = PaPart{b, len, (int)seg, (int)(local - seg * n), n, (int)place - (int)(local - seg * n), cut * segs + (int)seg};
+        break;
+      }
+      if (whole) ++at;
+      else { rec += n; ++cut; }
+    }
+  }
+  __syncthreads();
+  out = lds.mine;
+  return out.b >= 0;
 }
 
-constexpr int PA_WGS = 512;          // workgroups of a split launch: two of four waves fit a CU
-constexpr int PA_SPLIT_WAVES = 4, PA_JOIN_THREADS = 256;
-
-// A segment that is cut belongs to the piece in which it begins: cuts[piece], at most one per piece, tells the second launch
-// about it.  Where the call has fewer segments than pieces the entries are those of the segments instead (BY_PIECE false).
-template <typename T, int HD, bool BY_PIECE>
+template <typename T, int HD>
 __global__ __launch_bounds__(PA_SPLIT_WAVES * 64, 2) void page_attn_split_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
   extern __shared__ __align__(16) char pa_lds[];
-  __shared__ int scratch[PA_SPLIT_WAVES];
+  __shared__ PaCutLds cut_lds;
   const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, segs = a.kv_heads * a.q_blocks, wave_bytes = pa_wave_bytes<T, HD>(rows);
   char *own = pa_lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * wave_bytes;
-  int *before = reinterpret_cast<int *>(pa_lds + PA_SPLIT_WAVES * wave_bytes);
-  const PaCut c = pa_cut(a, PaGeo<T, HD>::TILE, segs, before, scratch);
-  for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {   // sequences without tokens
-    if (before[b + 1] != before[b]) continue;
-    for (int i = threadIdx.x; i < a.kv_heads * a.group * HD; i += PA_SPLIT_WAVES * 64) pa_finish<T>(a, b, i / HD, i % HD, 0.f, 0.f, 0.f);
-    if (!BY_PIECE)
-      for (int i = threadIdx.x; i < segs; i += PA_SPLIT_WAVES * 64) a.cuts[b * segs + i] = int4{0, 0, 0, 0};
+  PaPart found;
+  int cuts;
+  const bool any = pa_find_part<PaGeo<T, HD>::TILE>(a, segs, blockIdx.x, cut_lds, found, cuts);
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.cuts[0] = int4{cuts, 0, 0, 0};
+  if (!any) return;
+  // (uniform, but read from LDS)
+  const int b = __builtin_amdgcn_readfirstlane(found.b), len = __builtin_amdgcn_readfirstlane(found.len), seg = __builtin_amdgcn_readfirstlane(found.seg);
+  const int part = __builtin_amdgcn_readfirstlane(found.part), parts = __builtin_amdgcn_readfirstlane(found.parts), record = __builtin_amdgcn_readfirstlane(found.record);
+  const int h = a.q_blocks == 1 ? seg : seg / a.q_blocks, qb = seg - h * a.q_blocks;
+  const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
+  const int nt = (len + PaGeo<T, HD>::TILE - 1) / PaGeo<T, HD>::TILE;
+  int t0 = 0, t1 = nt;
+  if (parts > 1) {   // parts differ by a tile at most
+    const int base = nt / parts, more = nt - base * parts;
+    t0 = part * base + (part < more ? part : more);
+    t1 = t0 + base + (part < more ? 1 : 0);
+    if (part == 0 && threadIdx.x == 0) a.cuts[1 + found.cut] = int4{b, seg, record, parts};   // (the record of part 0)
   }
-  int64_t at = (int64_t)blockIdx.x * c.piece;
-  const int64_t end = at + c.piece < c.tiles ? at + c.piece : c.tiles;
-  int4 cut = {0, 0, 0, 0};
-  if (at < end) {
-    int b = pa_sequence(a, before, segs, at);
-    while (at < end) {
-      while ((int64_t)before[b + 1] * segs <= at) ++b;   // (ends: at < tiles)
-      const int nt = before[b + 1] - before[b];
-      const int64_t local = at - (int64_t)before[b] * segs;
-      const int seg = (int)pa_quotient(local, nt), t0 = (int)(local - (int64_t)seg * nt);
-      const int t1 = end - at < nt - t0 ? t0 + (int)(end - at) : nt;
-      const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
-      const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
-      PaState<T, HD> st;
-      pa_run<T, HD, PA_SPLIT_WAVES>(a, b, pa_len(a, b), h, h0, gq, t0, t1, own, st);
-      const int record = t0 == 0 && t1 == nt ? -1 : 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-      pa_join<T, HD, PA_SPLIT_WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, record);
-      if (t0 == 0) {
-        const int4 mine = {b, seg, (int)blockIdx.x, (int)pa_quotient(at + nt - 1, c.piece) - (int)blockIdx.x + 1};
-        if (t1 < nt) cut = mine;
-        if (!BY_PIECE && threadIdx.x == 0) a.cuts[b * segs + seg] = mine;
-      }
-      at += t1 - t0;
-      __syncthreads();
-    }
-  }
-  if (BY_PIECE && threadIdx.x == 0) a.cuts[blockIdx.x] = cut;
+  PaState<T, HD> st;
+  pa_run<T, HD, PA_SPLIT_WAVES>(a, b, len, h, h0, gq, t0, t1, own, st);
+  pa_join<T, HD, PA_SPLIT_WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, parts > 1 ? record + part : -1);
 }
 
-// Joins the records of a segment: one workgroup per piece that a cut segment begins in, or per segment and query head where
-// segments are few and their records many.  The beginning of a segment is its piece's second record, the rest are first
-// records, and they are added in this order.
+// Joins the records of a segment in their order: one workgroup per cut segment, or per query head of it where segments are few
+// and their records many.
 constexpr int PA_FEW = 4;   // records that a thread loads at once, weights and sums, in one trip to memory
 
-template <typename T, int HD, bool BY_PIECE>
+template <typename T, int HD, bool BY_HEAD>
 __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
   extern __shared__ __align__(16) char pa_lds[];
   __shared__ float tops[PA_MAX_Q], sums[PA_MAX_Q];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q;
-  const int4 cut = a.cuts[blockIdx.x];
-  const int b = cut.x, seg = cut.y, w0 = cut.z, n_rec = cut.w;
-  if (n_rec <= 1) return;    // no segment, or one workgroup had it all
+  const int n_cuts = a.cuts[0].x;
+  const int4 cut = a.cuts[1 + blockIdx.x];
+  if ((int)blockIdx.x >= n_cuts) return;
+  const int b = cut.x, seg = cut.y, n_rec = cut.w;
   const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
   const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
-  const int q0 = BY_PIECE ? 0 : blockIdx.y, nq = BY_PIECE ? gq : 1;
+  const int q0 = BY_HEAD ? blockIdx.y : 0, nq = BY_HEAD ? 1 : gq;
   if (q0 >= gq) return;
   constexpr int V = HD / 4;   // four elements a thread
   const int items = nq * V;
-  auto record = [&](int r) { return (int64_t)(2 * (w0 + r) + (r == 0 ? 1 : 0)) * rows + q0; };
+  auto record = [&](int r) { return (int64_t)(cut.z + r) * rows + q0; };
   auto finish = [&](int n, int d, float top, float sum, const float4 &o) {
     const float e[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
@@ -545,13 +605,26 @@ __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAtt
   }
 }
 
-constexpr int PA_WHOLE_TOKENS = 1024;
-constexpr unsigned PA_WIDE_SEGS = 256;
+// Launches of one workgroup per segment, or split ones?  The host knows a bound on the lengths, not the lengths.  us a call, whole
+// / split, 32 heads of 128 with 32 or 8 K/V heads, all sequences at the bound: 8 segments of 512 tokens 7.6 / 10.3, of 1100 14.9 /
+// 12.7; 32 of 512 9.7 / 12.0, of 1024 15.9 / 12.7; 128 of 512 12.0 / 14.5, of 1024 19.4 / 19.5, of 2048 32.3 / 30.8; 160 of 2048
+// 33.8 / 35.2; 192 36.8 / 42.7; 256 46.5 / 51.6; 512 86.5 / 89.1.  A long sequence among short ones is where whole segments lose,
+// 10 ns a token of the longest one at worst: 512 of 50 to 2000 tokens 57.7 / 54.7, 256 of 100 to 4000 60.1 / 61.0, 192 of 1 to 16000
+// 181 / 129.
+constexpr int PA_WHOLE_TOKENS = 768;
+constexpr unsigned PA_MANY_SEGS = 160;
+constexpr int PA_WHOLE_TOKENS_MANY = 2048;
+constexpr unsigned PA_JOIN_BY_HEAD = 256;
+constexpr size_t PA_JOIN_WEIGHTS = 8192;   // 32 KB of LDS
+
+// a segment of n parts has more than n - 1 times the tiles of a whole part, and n > 1: at most twice PA_PARTS records, of at most
+// PA_PARTS segments
+constexpr int PA_RECORDS = 2 * PA_PARTS;
 
 inline int pa_rows(const lightkv_pages *p) { const int g = p->heads / p->kv_heads; return g < PA_MAX_Q ? g : PA_MAX_Q; }
-inline size_t pa_stat_bytes(const lightkv_pages *p) { return ((size_t)2 * PA_WGS * pa_rows(p) * 2 * sizeof(float) + 255) / 256 * 256; }
-inline size_t pa_part_bytes(const lightkv_pages *p) { return (size_t)2 * PA_WGS * pa_rows(p) * p->head_dim * sizeof(float); }
-inline size_t pa_bytes(const lightkv_pages *p) { return pa_stat_bytes(p) + pa_part_bytes(p) + PA_WGS * sizeof(int4); }
+inline size_t pa_stat_bytes(const lightkv_pages *p) { return ((size_t)PA_RECORDS * pa_rows(p) * 2 * sizeof(float) + 255) / 256 * 256; }
+inline size_t pa_part_bytes(const lightkv_pages *p) { return (size_t)PA_RECORDS * pa_rows(p) * p->head_dim * sizeof(float); }
+inline size_t pa_bytes(const lightkv_pages *p) { return pa_stat_bytes(p) + pa_part_bytes(p) + (PA_PARTS + 1) * sizeof(int4); }
 
 template <typename T, int HD>
 static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t stream) {
@@ -559,22 +632,23 @@ static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t strea
   const size_t wave_bytes = pa_wave_bytes<T, HD>(rows);
   const unsigned segs = (unsigned)a.batch * (unsigned)(a.kv_heads * a.q_blocks);
   if (whole) {
-    if (rows <= 8 && segs <= PA_WIDE_SEGS) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), 8 * wave_bytes, stream, a);
+    if (rows <= 8) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), 8 * wave_bytes, stream, a);
     else hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 4>), dim3(segs), dim3(256), 4 * wave_bytes, stream, a);
     return hipGetLastError();
   }
-  const size_t list = ((size_t)a.batch + 1) * sizeof(int);   // of the sequences, behind the waves' LDS
-  const dim3 wgs(a.n_wgs), threads(PA_SPLIT_WAVES * 64);
-  const bool by_piece = segs >= (unsigned)a.n_wgs;
-  // records of a segment: all segments of a sequence are equally long, so n_wgs / (their number) + 2 at most
-  const size_t most = a.n_wgs / (size_t)(a.kv_heads * a.q_blocks) + 2;
-  const size_t join = (((by_piece ? rows : 1) * most + 3) / 4 * 4 + 4 * PA_JOIN_THREADS) * sizeof(float);
-  if (by_piece) hipLaunchKernelGGL((page_attn_split_kernel<T, HD, true>), wgs, threads, PA_SPLIT_WAVES * wave_bytes + list, stream, a);
-  else hipLaunchKernelGGL((page_attn_split_kernel<T, HD, false>), wgs, threads, PA_SPLIT_WAVES * wave_bytes + list, stream, a);
+  // parts: as many as a table row's tokens allow, PA_PARTS and one more per segment at most
+  const int64_t tile = PaGeo<T, HD>::TILE, longest = ((int64_t)a.room + tile * a.min_tiles - 1) / (tile * a.min_tiles);
+  const int64_t all = (int64_t)segs * longest < (int64_t)PA_PARTS + segs ? (int64_t)segs * longest : (int64_t)PA_PARTS + segs;
+  hipLaunchKernelGGL((page_attn_split_kernel<T, HD>), dim3((unsigned)all), dim3(PA_SPLIT_WAVES * 64), PA_SPLIT_WAVES * wave_bytes, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (by_piece) hipLaunchKernelGGL((page_attn_join_kernel<T, HD, true>), wgs, dim3(PA_JOIN_THREADS), join, stream, a);
-  else hipLaunchKernelGGL((page_attn_join_kernel<T, HD, false>), dim3(segs, rows), dim3(PA_JOIN_THREADS), join, stream, a);
+  const unsigned cuts = segs < (unsigned)PA_PARTS ? segs : (unsigned)PA_PARTS;
+  // records of a segment: those of a sequence's segments are as many, so PA_PARTS / (their number) + 1 at most
+  const size_t most = PA_PARTS / (size_t)(a.kv_heads * a.q_blocks) + 1;
+  const bool by_head = segs < PA_JOIN_BY_HEAD || rows * most > PA_JOIN_WEIGHTS;
+  const size_t join = (((by_head ? 1 : rows) * most + 3) / 4 * 4 + 4 * PA_JOIN_THREADS) * sizeof(float);
+  if (by_head) hipLaunchKernelGGL((page_attn_join_kernel<T, HD, true>), dim3(cuts, rows), dim3(PA_JOIN_THREADS), join, stream, a);
+  else hipLaunchKernelGGL((page_attn_join_kernel<T, HD, false>), dim3(cuts), dim3(PA_JOIN_THREADS), join, stream, a);
   return hipGetLastError();
 }
 
@@ -639,10 +713,10 @@ lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq
   a.o_tok = p->batch > 1 ? o_tok_stride * eb : 0; a.o_head = p->heads > 1 ? o_head_stride * eb : 0;
   a.batch = p->batch; a.kv_heads = p->kv_heads; a.group = p->heads / p->kv_heads; a.q_blocks = (a.group + PA_MAX_Q - 1) / PA_MAX_Q;
   a.n_pages = p->n_pages; a.lg = log2_of(p->page_tokens); a.room = p->max_pages * p->page_tokens;
-  a.n_wgs = PA_WGS; a.min_tiles = 8;
+  a.min_tiles = 8;
   a.scale2 = (softmax_scale > 0.f ? softmax_scale : 1.f / sqrtf((float)p->head_dim)) * PA_LOG2E;
   const int bound = max_seq_tokens > 0 && max_seq_tokens < a.room ? max_seq_tokens : a.room;
-  const bool whole = bound <= PA_WHOLE_TOKENS;
+  const bool whole = bound <= ((unsigned)(a.batch * a.kv_heads * a.q_blocks) < PA_MANY_SEGS ? PA_WHOLE_TOKENS : PA_WHOLE_TOKENS_MANY);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (p->dtype == LIGHTKV_BF16)
