@@ -60,15 +60,11 @@ template <typename T, int HD> struct PaTile {
 
 // K and V are read once (a group of more than 16 query heads aside) and are larger than the caches: loads that do not stay
 // there leave the memory more of its rate.  131000 tokens x 8 heads, 537 MB: 97 -> 86 us; 64 ragged sequences, 979 MB: 195 -> 181.
-__device__ __forceinline__ uint4 pa_ld16(const char *p) {
-  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)));
-}
 template <int W> __device__ __forceinline__ void pa_load_words(uint32_t (&d)[W], const char *p) {
   if constexpr (W % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < W; i += 4) {
-      const uint4 v = pa_ld16(p + i * 4);
+      const uint4 v = ld16_stream(p + i * 4);
       d[i] = v.x; d[i + 1] = v.y; d[i + 2] = v.z; d[i + 3] = v.w;
     }
   } else if constexpr (W == 2) {
@@ -201,16 +197,23 @@ __device__ __forceinline__ void pa_run(const PageAttnArgs &a, int b, int len, in
 #pragma unroll
   for (int t = 0; t < G::VT; ++t) st.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   int t = t0 + wave;
-  if (t >= t1) return;
   const int32_t *row = a.table + (int64_t)b * a.table_stride;
   const int in_page = (1 << a.lg) - 1;
-  // page of token lane % TILE of a tile; -1: does not count
-  auto pages_of = [&](int tile) {
-    const int key = tile * G::TILE + (lane & (G::TILE - 1));
-    int pg = -1;
-    if (key < len) pg = row[key >> a.lg];
-    return (unsigned)pg < (unsigned)a.n_pages ? pg : -1;
-  };
+  // table entry of token lane % TILE of a tile, and from it the token's page; -1: does not count
+  auto key_of = [&](int tile) { return tile * G::TILE + (lane & (G::TILE - 1)); };
+  auto entry_of = [&](int tile) { return key_of(tile) < a.room ? row[key_of(tile) >> a.lg] : -1; };
+  auto page_of = [&](int entry, int tile) { return key_of(tile) < len && (unsigned)entry < (unsigned)a.n_pages ? entry : -1; };
+  // queries and the first entries do not wait for the length
+  int next = entry_of(t);
+  uint4 q[G::KL];
+#pragma unroll
+  for (int i = 0; i < G::KL; ++i) q[i] = uint4{0u, 0u, 0u, 0u};
+  if (m < gq) {
+    const char *p = a.Q + (int64_t)b * a.q_tok + (int64_t)(h0 + m) * a.q_head + g * 16;
+#pragma unroll
+    for (int i = 0; i < G::KL; ++i) q[i] = ld16(p + i * 64);
+  }
+  if (t >= t1) return;
   // K: the lanes of a row side by side, KI tokens one behind the other for each; V: 16 lanes a row, NK tokens.  Either number
   // divides the smallest page, so the tokens of a lane share one.
   const int kr = lane / G::C;
@@ -222,34 +225,25 @@ __device__ __forceinline__ void pa_run(const PageAttnArgs &a, int b, int len, in
     const int kp = __shfl(safe, kr * G::KI, 64), vp = __shfl(safe, g * G::NK, 64);
     const char *p = kh + (int64_t)kp * a.k_page + (int64_t)((key0 + kr * G::KI) & in_page) * a.k_tok;
 #pragma unroll
-    for (int i = 0; i < G::KI; ++i) d.k[i] = pa_ld16(p + i * a.k_tok);
+    for (int i = 0; i < G::KI; ++i) d.k[i] = ld16_stream(p + i * a.k_tok);
     p = vh + (int64_t)vp * a.v_page + (int64_t)((key0 + g * G::NK) & in_page) * a.v_tok;
 #pragma unroll
     for (int i = 0; i < G::NK; ++i) pa_load_words<G::VW>(d.v[i], p + i * a.v_tok);
   };
-  uint4 q[G::KL];
-#pragma unroll
-  for (int i = 0; i < G::KL; ++i) q[i] = uint4{0u, 0u, 0u, 0u};
-  if (m < gq) {
-    const char *p = a.Q + (int64_t)b * a.q_tok + (int64_t)(h0 + m) * a.q_head + g * 16;
-#pragma unroll
-    for (int i = 0; i < G::KL; ++i) q[i] = ld16(p + i * 64);
-  }
   PaTile<T, HD> x, y;
-  int next = pages_of(t);
-  load(x, t, next);
-  next = pages_of(t + WAVES < t1 ? t + WAVES : t);
+  load(x, t, page_of(next, t));
+  next = t + WAVES < t1 ? entry_of(t + WAVES) : -1;
   for (;;) {
     if (t + WAVES < t1) {
-      load(y, t + WAVES, next);
-      next = pages_of(t + 2 * WAVES < t1 ? t + 2 * WAVES : t);
+      load(y, t + WAVES, page_of(next, t + WAVES));
+      next = t + 2 * WAVES < t1 ? entry_of(t + 2 * WAVES) : -1;
     }
     pa_accumulate<T, HD>(st, x, q, a.scale2, lds);
     t += WAVES;
     if (t >= t1) break;
     if (t + WAVES < t1) {
-      load(x, t + WAVES, next);
-      next = pages_of(t + 2 * WAVES < t1 ? t + 2 * WAVES : t);
+      load(x, t + WAVES, page_of(next, t + WAVES));
+      next = t + 2 * WAVES < t1 ? entry_of(t + 2 * WAVES) : -1;
     }
     pa_accumulate<T, HD>(st, y, q, a.scale2, lds);
     t += WAVES;
@@ -329,7 +323,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_whole_kernel(PageAttn
   const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q, wave_bytes = pa_wave_bytes<T, HD>(rows);
   char *own = pa_lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * wave_bytes;
   const int segs = a.kv_heads * a.q_blocks, b = blockIdx.x / segs, seg = blockIdx.x - b * segs;
-  const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
+  const int h = a.q_blocks == 1 ? seg : seg / a.q_blocks, qb = seg - h * a.q_blocks;
   const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
   const int len = pa_len(a, b);
   PaState<T, HD> st;
@@ -348,28 +342,6 @@ constexpr int PA_PARTS = 1024, PA_SLOTS = 512, PA_FEW_SEGS = 192;
 // Quotient of numbers that are small in all but impossible calls: a 64-bit division is 130 instructions.
 __device__ __forceinline__ int64_t pa_quotient(int64_t n, int64_t d) {
   return ((n | d) >> 32) == 0 ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
-}
-
-// Inclusive running sum over the wave.
-__device__ __forceinline__ int wave_running_sum(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8: inside rows of 16 lanes
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // lane 15 of a row to the next row: rows 1 and 3
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2 and 3
-  return v;
-}
-
-__device__ __forceinline__ int wave_running_max(int v) {   // of numbers that are not negative
-  auto larger = [](int x, int y) { return x > y ? x : y; };
-  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
-  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
-  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
-  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
-  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
-  v = larger(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
-  return v;
 }
 
 // What a workgroup of a split launch has to do: part `part` of `parts` of segment `seg` of sequence b.
@@ -612,6 +584,9 @@ __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAtt
 // 10 ns a token of the longest one at worst: 512 of 50 to 2000 tokens 57.7 / 54.7, 256 of 100 to 4000 60.1 / 61.0, 192 of 1 to 16000
 // 181 / 129.
 constexpr int PA_WHOLE_TOKENS = 768;
+// Eight waves a segment where each has a CU of its own, four where two share one.  us, eight / four: 32 segments of 381 tokens 6.5 / 7.5,
+// 240 of 1850 41.5 / 42.7, 2048 of 256 55.1 / 47.7.  (More than eight query heads: the join of eight waves would not fit the LDS.)
+constexpr unsigned PA_WIDE_SEGS = 256;
 constexpr unsigned PA_MANY_SEGS = 160;
 constexpr int PA_WHOLE_TOKENS_MANY = 2048;
 constexpr unsigned PA_JOIN_BY_HEAD = 256;
@@ -632,7 +607,7 @@ static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t strea
   const size_t wave_bytes = pa_wave_bytes<T, HD>(rows);
   const unsigned segs = (unsigned)a.batch * (unsigned)(a.kv_heads * a.q_blocks);
   if (whole) {
-    if (rows <= 8) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), 8 * wave_bytes, stream, a);
+    if (rows <= 8 && segs <= PA_WIDE_SEGS) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), 8 * wave_bytes, stream, a);
     else hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 4>), dim3(segs), dim3(256), 4 * wave_bytes, stream, a);
     return hipGetLastError();
   }

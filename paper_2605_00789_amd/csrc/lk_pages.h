@@ -1,7 +1,8 @@
-// What the calls of the paged cache share on the host: checks of the descriptor.
+// What the calls of the paged cache share: checks of the descriptor (host), loads and running sums (device).
 #pragma once
 #include "../../include/lightkv.h"
 
+#include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -70,5 +71,24 @@ inline uint64_t pool_bytes(const lightkv_pages *p, int64_t page_stride, int64_t 
   return strided_bytes(page_elem_bytes(p), page_stride, p->n_pages, head_stride, p->kv_heads, p->head_dim)
          + (uint64_t)tok_stride * (uint64_t)(p->page_tokens - 1) * (uint64_t)page_elem_bytes(p);
 }
+
+// ---- device ----
+// Loads and stores of memory that is touched once: they do not stay in the caches.
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+__device__ __forceinline__ uint4 ld16_stream(const char *p) { return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p))); }
+__device__ __forceinline__ void st16_stream(char *p, const uint4 &v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4 *>(p)); }
+
+// Inclusive running result of `op` over the lanes of a wave, for an op with 0 as its neutral element.
+template <typename Op> __device__ __forceinline__ int wave_running(int v, Op op) {
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));   // row_shr 1, 2, 4, 8: inside rows of 16 lanes
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));   // lane 15 of a row to the next row: rows 1 and 3
+  v = op(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));   // lane 31 to rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ int wave_running_sum(int v) { return wave_running(v, [](int a, int b) { return a + b; }); }
+__device__ __forceinline__ int wave_running_max(int v) { return wave_running(v, [](int a, int b) { return a > b ? a : b; }); }   // (not negative)
 
 }  // namespace lk

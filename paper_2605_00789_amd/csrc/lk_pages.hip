@@ -15,7 +15,7 @@ namespace lk {
 
 constexpr int PG_THREADS = 256;
 constexpr int PG_SLOTS_PER_THREAD = 4;     // one 16-byte store
-constexpr int PG_MAX_WGS = 512;
+constexpr int PG_MAX_WGS = 1536;
 constexpr int PG_SAT = 1 << 29;            // sums of impossible lengths stop here: above any number of pages
 
 struct AllocArgs {
@@ -31,12 +31,7 @@ __device__ __forceinline__ int sat_add(int a, int b) { const int s = a + b; retu
 // Exclusive running sum (saturating) of one number per thread over the workgroup; *total is the sum of all.
 __device__ __forceinline__ int wg_exclusive_sum(int v, int *scratch, int *total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int incl = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(incl, o, 64);
-    if (lane >= o) incl = sat_add(incl, u);
-  }
+  int incl = wave_running(v, sat_add);
   if (lane == 63) scratch[wave] = incl;
   __syncthreads();
   int base = 0, sum = 0;
@@ -46,8 +41,7 @@ __device__ __forceinline__ int wg_exclusive_sum(int v, int *scratch, int *total)
     sum = sat_add(sum, scratch[w]);
   }
   *total = sum;
-  const int before = __shfl_up(incl, 1, 64);
-  return lane == 0 ? base : sat_add(base, before);
+  return sat_add(base, __builtin_amdgcn_update_dpp(0, incl, 0x138, 0xf, 0xf, false));   // wave_shr 1
 }
 
 // Last index i in [0, n) with list[i] <= v (list ascending, list[0] <= v).
@@ -59,6 +53,18 @@ __device__ __forceinline__ int last_not_above(const int *list, int n, int v) {
     else hi = mid;
   }
   return lo;
+}
+
+// n ints into LDS by the whole workgroup, four loads of a thread at a time.
+__device__ __forceinline__ void pg_fetch(const int32_t *from, int *to, int n) {
+  for (int i0 = threadIdx.x; i0 < n; i0 += 4 * PG_THREADS) {
+    int v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = i0 + u * PG_THREADS < n ? from[i0 + u * PG_THREADS] : 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u * PG_THREADS < n) to[i0 + u * PG_THREADS] = v[u];
+  }
 }
 
 __device__ __forceinline__ int clamped_count(const int32_t *count, int n_pages) {
@@ -76,12 +82,13 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
   const int tid = threadIdx.x, count = clamped_count(g.free_count, g.n_pages);
   const int room = g.max_pages << g.lg, P = 1 << g.lg;
   const int per = (g.batch + PG_THREADS - 1) / PG_THREADS, b0 = tid * per, b1 = b0 + per < g.batch ? b0 + per : g.batch;
-  if (tid == 0) { popped = 0; cu[g.batch] = g.cu_new[g.batch]; }
+  if (tid == 0) popped = 0;
+  pg_fetch(g.cu_new, cu, g.batch + 1);
+  pg_fetch(g.seq_lens, len, g.batch);
+  __syncthreads();
   int mine = 0;
   for (int b = b0; b < b1; ++b) {
-    const int first = g.cu_new[b], end = g.cu_new[b + 1], L = g.seq_lens[b];
-    cu[b] = first;
-    len[b] = L;
+    const int first = cu[b], end = cu[b + 1], L = len[b];
     // (differences of any two ints: 64 bits)
     const int64_t n = (int64_t)end - first;
     const bool over = first < 0 || n < 0 || end > g.slot_rows || L < 0 || L + n > room;
@@ -90,14 +97,18 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
     mine = sat_add(mine, need);
   }
   int total;
-  int at = wg_exclusive_sum(mine, scratch, &total);
+  int at = wg_exclusive_sum(mine, scratch, &total), served = 0;
   for (int b = b0; b < b1; ++b) {
     const int need = place[b];
     if (need < 0) continue;
     const bool ok = need == 0 || sat_add(at, need) <= count;
     place[b] = ok ? at : -1;
     at = sat_add(at, need);
-    if (ok && need > 0) atomicMax(&popped, at);
+    if (ok && need > 0) served = at;
+  }
+  if ((g.what & 2) && blockIdx.x == 0) {
+    served = wave_running_max(served);
+    if ((tid & 63) == 63) atomicMax(&popped, served);
   }
   __syncthreads();
   if ((g.what & 2) && blockIdx.x == 0) {
@@ -113,7 +124,7 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
   const int64_t step = (int64_t)gridDim.x * PG_THREADS * PG_SLOTS_PER_THREAD;
   const bool wide = (reinterpret_cast<uintptr_t>(g.slots) & 15) == 0;
   for (int64_t t0 = ((int64_t)blockIdx.x * PG_THREADS + tid) * PG_SLOTS_PER_THREAD; t0 < end; t0 += step) {
-    int b = 0, out[PG_SLOTS_PER_THREAD];
+    int b = 0, page = -1, page_j = -1, page_b = -1, out[PG_SLOTS_PER_THREAD];
     unsigned have = 0;
     if (cu[0] <= t0) b = last_not_above(cu, g.batch, (int)t0);
 #pragma unroll
@@ -126,13 +137,12 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
       have |= 1u << i;
       if (place[b] < 0) continue;
       const int L = len[b], pos = L + (int)(t - cu[b]), j = pos >> g.lg, old = (L + P - 1) >> g.lg;
-      int page;
-      if (j < old) {
-        page = g.table[(int64_t)b * g.table_stride + j];
-      } else {
-        page = g.free_pages[count - 1 - (place[b] + j - old)];
-        if ((pos & (P - 1)) == 0) g.table[(int64_t)b * g.table_stride + j] = page;
+      if (j != page_j || b != page_b) {   // (mostly one page for the slots of a thread: one trip to memory)
+        page = j < old ? g.table[(int64_t)b * g.table_stride + j] : g.free_pages[count - 1 - (place[b] + j - old)];
+        page_j = j;
+        page_b = b;
       }
+      if (j >= old && (pos & (P - 1)) == 0) g.table[(int64_t)b * g.table_stride + j] = page;
       if ((unsigned)page < (unsigned)g.n_pages) out[i] = (page << g.lg) + (pos & (P - 1));
     }
     if (wide && have == (1u << PG_SLOTS_PER_THREAD) - 1) {
@@ -153,7 +163,7 @@ struct FreeArgs {
   int what;   // 1: the stack, 2: lengths and count
 };
 
-// LDS: pages pushed before sequence b [batch]
+// LDS: flag, then pages pushed before sequence b [batch]; length [batch]
 __global__ __launch_bounds__(PG_THREADS) void page_free_kernel(FreeArgs g) {
   fetch_args<FreeArgs>();
   extern __shared__ int pg_lds[];
@@ -161,11 +171,15 @@ __global__ __launch_bounds__(PG_THREADS) void page_free_kernel(FreeArgs g) {
   int *before = pg_lds;
   const int tid = threadIdx.x, count = clamped_count(g.free_count, g.n_pages), P = 1 << g.lg;
   const int per = (g.batch + PG_THREADS - 1) / PG_THREADS, b0 = tid * per, b1 = b0 + per < g.batch ? b0 + per : g.batch;
+  int *len = before + g.batch;
+  pg_fetch(g.seq_lens, len, g.batch);
+  pg_fetch(g.done, before, g.batch);
+  __syncthreads();
   int mine = 0;
   for (int b = b0; b < b1; ++b) {
-    const int L = g.seq_lens[b];
+    const int L = len[b];
     int held = 0;
-    if (g.done[b] != 0 && L > 0) {
+    if (before[b] != 0 && L > 0) {
       held = (int)(((int64_t)L + P - 1) >> g.lg);
       held = held < g.max_pages ? held : g.max_pages;
     }
@@ -182,7 +196,7 @@ __global__ __launch_bounds__(PG_THREADS) void page_free_kernel(FreeArgs g) {
   __syncthreads();
   const int room = g.n_pages - count, pushed = total < room ? total : room;
   if ((g.what & 2) && blockIdx.x == 0) {
-    for (int b = tid; b < g.batch; b += PG_THREADS) g.seq_lens_out[b] = g.done[b] != 0 ? 0 : g.seq_lens[b];
+    for (int b = tid; b < g.batch; b += PG_THREADS) g.seq_lens_out[b] = g.done[b] != 0 ? 0 : len[b];
     if (tid == 0) g.free_count_out[0] = count + pushed;
   }
   if (!(g.what & 1)) return;
@@ -194,6 +208,11 @@ __global__ __launch_bounds__(PG_THREADS) void page_free_kernel(FreeArgs g) {
 
 // Rows into pages: both streams of rows are read and written once, so the time is that of a copy.  A workgroup takes whole rows
 // of K (blockIdx.y 0) or V (1), 16 bytes a thread and trip.
+constexpr int PG_WRITE_U = 4;
+// Rows of more than the L2 caches hold pass them by, in and out.  us a call, through the caches / past them: 121 MB of rows 46.9 / 43.0,
+// 262 MB 100.2 / 96.3; 19 MB 8.2 / 8.9, 4 MB 3.7 / 4.0.
+constexpr uint64_t PG_STREAM_BYTES = 32u << 20;
+
 struct WriteArgs {
   const int32_t *cu_new, *slots;
   const char *src[2];
@@ -205,6 +224,7 @@ struct WriteArgs {
   int rows_per_wg;
 };
 
+template <bool STREAM>
 __global__ __launch_bounds__(PG_THREADS) void page_write_kernel(WriteArgs g) {
   fetch_args<WriteArgs>();
   const int y = blockIdx.y;
@@ -213,13 +233,28 @@ __global__ __launch_bounds__(PG_THREADS) void page_write_kernel(WriteArgs g) {
   const int per = g.pieces_per_row, in_head = (1 << g.lg_pieces) - 1;
   for (int64_t r0 = (int64_t)blockIdx.x * g.rows_per_wg; r0 < rows; r0 += (int64_t)gridDim.x * g.rows_per_wg) {
     const int n_rows = rows - r0 < g.rows_per_wg ? (int)(rows - r0) : g.rows_per_wg;
-    for (int i = threadIdx.x; i < n_rows * per; i += PG_THREADS) {
-      const int r = i / per, piece = i - r * per, head = piece >> g.lg_pieces;
-      const int slot = g.slots[r0 + r];
-      if ((unsigned)slot >= (unsigned)g.n_slots) continue;
-      const uint4 v = ld16(g.src[y] + (r0 + r) * g.src_tok[y] + head * g.src_head[y] + (piece & in_head) * 16);
-      char *to = g.dst[y] + (int64_t)(slot >> g.lg) * g.dst_page[y] + (int64_t)(slot & ((1 << g.lg) - 1)) * g.dst_tok[y] + head * g.dst_head[y] + (piece & in_head) * 16;
-      *reinterpret_cast<uint4 *>(to) = v;
+    // all loads of a thread are on their way before the first store
+    for (int i0 = threadIdx.x; i0 < n_rows * per; i0 += PG_THREADS * PG_WRITE_U) {
+      uint4 v[PG_WRITE_U];
+      int slot[PG_WRITE_U], head[PG_WRITE_U], piece[PG_WRITE_U];
+#pragma unroll
+      for (int u = 0; u < PG_WRITE_U; ++u) {
+        const int i = i0 + u * PG_THREADS, r = i / per, k = i - r * per;
+        head[u] = k >> g.lg_pieces;
+        piece[u] = (k & in_head) * 16;
+        slot[u] = -1;
+        if (i < n_rows * per) slot[u] = g.slots[r0 + r];
+        v[u] = uint4{0u, 0u, 0u, 0u};
+        const char *from = g.src[y] + (r0 + r) * g.src_tok[y] + head[u] * g.src_head[y] + piece[u];
+        if (i < n_rows * per) v[u] = STREAM ? ld16_stream(from) : ld16(from);
+      }
+#pragma unroll
+      for (int u = 0; u < PG_WRITE_U; ++u) {
+        if ((unsigned)slot[u] >= (unsigned)g.n_slots) continue;
+        char *to = g.dst[y] + (int64_t)(slot[u] >> g.lg) * g.dst_page[y] + (int64_t)(slot[u] & ((1 << g.lg) - 1)) * g.dst_tok[y] + head[u] * g.dst_head[y] + piece[u];
+        if (STREAM) st16_stream(to, v[u]);
+        else *reinterpret_cast<uint4 *>(to) = v[u];
+      }
     }
   }
 }
@@ -298,9 +333,9 @@ lightkv_status lightkv_page_free(const lightkv_pages *p, const int32_t *done, co
   g.done = done; g.seq_lens = seq_lens; g.free_pages = free_pages; g.free_count = free_count; g.table = p->table;
   g.seq_lens_out = seq_lens_out; g.free_count_out = free_count_out; g.table_stride = p->table_stride; g.batch = p->batch;
   g.max_pages = p->max_pages; g.n_pages = p->n_pages; g.lg = log2_of(p->page_tokens);
-  const size_t lds = (size_t)p->batch * sizeof(int);
+  const size_t lds = 2 * (size_t)p->batch * sizeof(int);
   const int64_t most = (int64_t)p->batch * p->max_pages < p->n_pages ? (int64_t)p->batch * p->max_pages : p->n_pages;
-  const int64_t want = (most + PG_THREADS * 4 - 1) / (PG_THREADS * 4);
+  const int64_t want = (most + PG_THREADS * 2 - 1) / (PG_THREADS * 2);
   const int wgs = (int)(want < 1 ? 1 : (want > PG_MAX_WGS ? PG_MAX_WGS : want));
   const bool in_place = seq_lens_out == seq_lens || free_count_out == free_count;
   g.what = wgs > 1 && in_place ? 1 : 3;
@@ -349,7 +384,9 @@ lightkv_status lightkv_page_write(const lightkv_pages *p, const int32_t *cu_new,
   g.pieces_per_row = p->kv_heads << g.lg_pieces;
   g.rows_per_wg = g.pieces_per_row < 1024 ? 1024 / g.pieces_per_row : 1;
   const int64_t want = (rows + g.rows_per_wg - 1) / g.rows_per_wg, wgs = want < (1 << 20) ? want : (1 << 20);
-  hipLaunchKernelGGL(page_write_kernel, dim3((unsigned)wgs, (unsigned)n), dim3(PG_THREADS), 0, static_cast<hipStream_t>(stream), g);
+  const bool stream_through = (uint64_t)rows * g.pieces_per_row * 16 * n >= PG_STREAM_BYTES;
+  const auto kernel = stream_through ? page_write_kernel<true> : page_write_kernel<false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs, (unsigned)n), dim3(PG_THREADS), 0, static_cast<hipStream_t>(stream), g);
   return hipGetLastError() == hipSuccess ? LIGHTKV_OK : LIGHTKV_ERR_LAUNCH;
 }
 
