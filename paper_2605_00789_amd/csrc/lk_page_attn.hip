@@ -164,7 +164,9 @@ __device__ __forceinline__ void pa_accumulate(PaState<T, HD> &st, PaTile<T, HD> 
     for (int j = 0; j < 4; ++j) {
       const uint32_t a = __float_as_uint(p[j >> 1][(j & 1) * 2]), b = __float_as_uint(p[j >> 1][(j & 1) * 2 + 1]);
       hi[j] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-      const float ra = __uint_as_float(a) - __uint_as_float(a & 0xffff0000u), rb = __uint_as_float(b) - __uint_as_float(b & 0xffff0000u);
+      // (a little more than the rest: a weight that one bf16 number holds must not meet an infinity with a zero)
+      const float ra = fmaf(p[j >> 1][(j & 1) * 2], 0x1p-24f, __uint_as_float(a) - __uint_as_float(a & 0xffff0000u));
+      const float rb = fmaf(p[j >> 1][(j & 1) * 2 + 1], 0x1p-24f, __uint_as_float(b) - __uint_as_float(b & 0xffff0000u));
       lo[j] = __builtin_amdgcn_perm(__float_as_uint(rb), __float_as_uint(ra), 0x07060302u);
     }
     const bf16x8 ph = __builtin_bit_cast(bf16x8, uint4{hi[0], hi[1], hi[2], hi[3]}), pl = __builtin_bit_cast(bf16x8, uint4{lo[0], lo[1], lo[2], lo[3]});
@@ -671,8 +673,8 @@ lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq
   const uint64_t k_bytes = pool_bytes(p, p->k_page_stride, p->k_tok_stride, p->k_head_stride), v_bytes = pool_bytes(p, p->v_page_stride, p->v_tok_stride, p->v_head_stride);
   if (overlap(p->K, k_bytes, out, out_bytes) || overlap(p->V, v_bytes, out, out_bytes) || overlap(ws, ws_bytes, out, out_bytes)) return LIGHTKV_ERR_SHAPE;
   // rows of the output must not share elements
-  if (p->heads > 1 && o_head_stride < p->head_dim) return LIGHTKV_ERR_SHAPE;
-  if (p->batch > 1 && o_tok_stride < p->head_dim) return LIGHTKV_ERR_SHAPE;
+  const int64_t o_stride[2] = {o_tok_stride, o_head_stride}, o_count[2] = {p->batch, p->heads};
+  if (!apart(p->head_dim, o_stride, o_count, 2)) return LIGHTKV_ERR_SHAPE;
   const size_t stat = pa_stat_bytes(p);
   if (!ws || !aligned_to(ws, 256) || ws_bytes < pa_bytes(p)) return LIGHTKV_ERR_WORKSPACE;
   PageAttnArgs a{};

@@ -41,6 +41,22 @@ inline uint64_t strided_bytes(int elem_bytes, int64_t outer, int64_t n_outer, in
   return ((uint64_t)(n_outer > 1 ? outer : 0) * (uint64_t)(n_outer - 1) + (uint64_t)(heads > 1 ? head : 0) * (uint64_t)(heads - 1) + (uint64_t)head_dim) * (uint64_t)elem_bytes;
 }
 
+// Whether rows of `run` elements at the given strides (of axes with more than one entry) are apart, axis within axis.
+inline bool apart(int64_t run, const int64_t *stride, const int64_t *count, int axes) {
+  int64_t extent = run;
+  bool done[3] = {};
+  for (int k = 0; k < axes; ++k) {
+    int next = -1;
+    for (int i = 0; i < axes; ++i)
+      if (!done[i] && count[i] > 1 && (next < 0 || stride[i] < stride[next])) next = i;
+    if (next < 0) break;
+    if (stride[next] < extent) return false;
+    done[next] = true;
+    extent += stride[next] * (count[next] - 1);
+  }
+  return true;
+}
+
 inline bool overlap(const void *a, uint64_t na, const void *b, uint64_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return a && b && x < y + nb && y < x + na;

@@ -365,6 +365,9 @@ lightkv_status lightkv_page_write(const lightkv_pages *p, const int32_t *cu_new,
     if (!src[i]) continue;
     st = check_strided(src[i], eb, tok[i], rows, head[i], p->kv_heads);
     if (st != LIGHTKV_OK) return st;
+    // rows of a pool that is written must not share elements
+    const int64_t stride[3] = {page_s[i], tok_s[i], head_s[i]}, count[3] = {p->n_pages, p->page_tokens, p->kv_heads};
+    if (!apart(p->head_dim, stride, count, 3)) return LIGHTKV_ERR_SHAPE;
     const uint64_t n = strided_bytes(eb, tok[i], rows, head[i], p->kv_heads, p->head_dim);
     for (int k = 0; k < 2; ++k)
       if (src[k] && overlap(src[i], n, dst[k], pool_bytes(p, page_s[k], tok_s[k], head_s[k]))) return LIGHTKV_ERR_SHAPE;

@@ -373,6 +373,71 @@ def test_attention_of_extreme_rows(dtype, hint):
     assert torch.isnan(out[7, 0]).all()
 
 
+@pytest.mark.parametrize("hint", [1, 1 << 20], ids=["whole", "split"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_infinite_values_under_round_weights(dtype, hint):
+    """A weight of 1, of 1/2, of 1/4: numbers that a bf16 value holds exactly, against rows with infinities."""
+    from paper_2605_00789_amd import binding as B
+    D, P, dt = 32, 8, TORCH[dtype]
+    lens, inf = [1, 2, 4, 4], float("inf")
+    K, V = (torch.zeros(4, P, 1, D, dtype=dt, device=DEV) for _ in range(2))
+    V[:, :, :, 1] = 3.0
+    V[:, 0, :, 0], V[1, 1, :, 2], V[3, 1, :, 0] = inf, -inf, -inf
+    Q, out = torch.ones(4, 1, D, dtype=dt, device=DEV), torch.empty(4, 1, D, dtype=dt, device=DEV)
+    attend(B, B.Pages(ints([[0], [1], [2], [3]]), K=K, V=V, heads=1), lens, Q, out, max_seq_tokens=hint)
+    want = torch.zeros(4, D)
+    want[:, 0], want[:, 1], want[1, 2], want[3, 0] = inf, 3.0, -inf, float("nan")
+    assert torch.equal(out[:, 0].float().cpu().nan_to_num(nan=77.0, posinf=1e30, neginf=-1e30), want.nan_to_num(nan=77.0, posinf=1e30, neginf=-1e30))
+
+
+@pytest.mark.parametrize("batch,H,group,D,dtype,lens", [
+    (700, 1, 2, 32, "bf16", (0, 90)), (300, 2, 1, 64, "f32", (1, 60)), (4096, 1, 1, 32, "bf16", (0, 20)), (257, 4, 3, 32, "bf16", (60, 64)),
+    (1100, 1, 1, 32, "f32", (0, 30)), (65, 8, 1, 64, "bf16", (100, 700))])
+def test_attention_of_large_batches(batch, H, group, D, dtype, lens):
+    """More sequences than threads that look for a part, a long sequence among short ones, more segments than workgroups fit."""
+    print("[batch]", batch, H, group, D, dtype, lens, flush=True)
+    from paper_2605_00789_amd import binding as B
+    P, rng = 16, random.Random(batch)
+    n = [rng.randint(*lens) for _ in range(batch)]
+    for long in (None, 3, batch - 1):
+        if long is not None:
+            n[long] = 3001
+        width = -(-max(n) // P)
+        n_pages = sum(-(-v // P) for v in n) + 2
+        K, V = (pool(n_pages, P, H, D, TORCH[dtype], "head", seed=s) for s in (1, 2))
+        table, _ = scattered(n, P, n_pages, width, 5)
+        Q = torch.randn(batch, H * group, D, generator=torch.Generator().manual_seed(7)).to(TORCH[dtype]).to(DEV)
+        out, lse = torch.empty_like(Q), torch.empty(H * group, batch, device=DEV)
+        attend(B, B.Pages(ints(table), K=K, V=V, heads=H * group), n, Q, out, lse, max_seq_tokens=1 << 20)
+        check(dtype, out, lse, reference(Q, K, V, table, n, P, D ** -0.5), D, n)
+
+
+def test_a_captured_split_follows_the_lengths():
+    """One graph, replayed while sequences grow from nothing to thousands of tokens and shrink again: the cut is the device's."""
+    from paper_2605_00789_amd import binding as B
+    H, group, D, P, batch, room = 2, 4, 64, 16, 5, 6000
+    n_pages = batch * room // P
+    K, V = (pool(n_pages, P, H, D, torch.bfloat16, "head", seed=s) for s in (1, 2))
+    table = [random.Random(9).sample(range(n_pages), n_pages)[b::batch] for b in range(batch)]
+    pages = B.Pages(ints(table), K=K, V=V, heads=H * group)
+    ws = torch.empty(B.lightkv_page_attention_workspace(pages), dtype=torch.uint8, device=DEV).fill_(0xff)
+    lens = ints([0] * batch)
+    Q = torch.randn(batch, H * group, D, device=DEV).to(torch.bfloat16)
+    out, lse = torch.zeros_like(Q), torch.zeros(H * group, batch, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.lightkv_page_attention(pages, lens, Q, out, ws, lse=lse)
+    for n in ([0] * 5, [1, 2, 3, 4, 5], [5990, 0, 40, 1000, 1], [2000] * 5, [6000, 6000, 6000, 6000, 0], [0, 0, 700, 0, 0]):
+        lens.copy_(ints(n))
+        graph.replay()
+        check("bf16", out, lse, reference(Q, K, V, table, n, P, D ** -0.5), D, n)
+        ws.fill_(0xff)
+        graph.replay()
+        check("bf16", out, lse, reference(Q, K, V, table, n, P, D ** -0.5), D, n)
+        torch.randn(1000, device=DEV).sum().item()
+
+
 def test_attention_of_a_row_does_not_depend_on_where_its_pages_lie():
     from paper_2605_00789_amd import binding as B
     H, D, P, n = 2, 128, 16, 333

@@ -122,6 +122,22 @@ def test_write_arguments(B):
     assert _write(B, p, K=at(1) + 256) == SHAPE and _write(B, p, V=at(1)) == SHAPE and _write(B, p, K=at(2) + 10 * 16 * 256 - 32) == SHAPE
 
 
+def test_rows_that_share_elements(B):
+    """Where a call writes, rows may be in any order but not in each other."""
+    for over in (dict(k_tok_stride=64), dict(k_head_stride=32), dict(v_tok_stride=0), dict(k_page_stride=1024), dict(v_head_stride=64), dict(v_page_stride=0)):
+        assert _write(B, _pages(B, **over)) == SHAPE, over
+    # heads outermost, tokens outermost, one page, gaps: all fine (no rows: nothing is launched)
+    for over in (dict(k_head_stride=10 * 16 * 64, k_page_stride=16 * 64, k_tok_stride=64), dict(k_tok_stride=10 * 128, k_page_stride=128),
+                 dict(n_pages=1, k_page_stride=0, v_page_stride=8), dict(k_page_stride=8192, k_tok_stride=256, k_head_stride=72)):
+        assert _write(B, _pages(B, **over), rows=0) == OK, over
+    p = _pages(B)
+    for o in (dict(ot=64, oh=128), dict(ot=512, oh=32), dict(ot=448, oh=64), dict(ot=64, oh=64), dict(ot=0), dict(oh=0)):
+        assert _attend(B, p, **o) == SHAPE, o
+    assert _attend(B, p, ot=64, oh=3 * 64, ws=None) == WORKSPACE       # heads outermost: past this check
+    # where a pool is only read, its rows may be one and the same
+    assert _attend(B, _pages(B, k_tok_stride=0, v_page_stride=0), ws=None) == WORKSPACE
+
+
 def test_attention_arguments(B):
     p = _pages(B)
     for name in ("lens", "Q", "out"):
