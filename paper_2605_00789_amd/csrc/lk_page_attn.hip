@@ -58,20 +58,25 @@ template <typename T, int HD> struct PaTile {
   uint32_t live;                                   // bit t: token t of the tile counts
 };
 
-// K and V are read once (a group of more than 16 query heads aside) and are larger than the caches: loads that do not stay
-// there leave the memory more of its rate.  131000 tokens x 8 heads, 537 MB: 97 -> 86 us; 64 ragged sequences, 979 MB: 195 -> 181.
-template <int W> __device__ __forceinline__ void pa_load_words(uint32_t (&d)[W], const char *p) {
+// ONCE: K and V are read by one workgroup each and are larger than the caches: loads that do not stay there leave the memory more
+// of its rate.  131000 tokens x 8 heads, 537 MB: 97 -> 86 us; 64 ragged sequences, 979 MB: 195 -> 181.  Blocks of a larger
+// group of query heads find each other's rows in the caches: 4 x 30000 tokens, 128 heads over one, 51.0 us past them and 35.8
+// through them; 16 x 8192, 128 over 4, 93.6 and 88.3.
+template <bool ONCE> __device__ __forceinline__ uint4 pa_ld16(const char *p) { return ONCE ? ld16_stream(p) : ld16(p); }
+template <int W, bool ONCE> __device__ __forceinline__ void pa_load_words(uint32_t (&d)[W], const char *p) {
   if constexpr (W % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < W; i += 4) {
-      const uint4 v = ld16_stream(p + i * 4);
+      const uint4 v = pa_ld16<ONCE>(p + i * 4);
       d[i] = v.x; d[i + 1] = v.y; d[i + 2] = v.z; d[i + 3] = v.w;
     }
   } else if constexpr (W == 2) {
-    const uint64_t v = __builtin_nontemporal_load(reinterpret_cast<const uint64_t *>(p));
+    const uint64_t *q = reinterpret_cast<const uint64_t *>(p);
+    const uint64_t v = ONCE ? __builtin_nontemporal_load(q) : *q;
     d[0] = (uint32_t)v; d[1] = (uint32_t)(v >> 32);
   } else {
-    d[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p));
+    const uint32_t *q = reinterpret_cast<const uint32_t *>(p);
+    d[0] = ONCE ? __builtin_nontemporal_load(q) : *q;
   }
 }
 
@@ -190,7 +195,7 @@ __device__ __forceinline__ void pa_accumulate(PaState<T, HD> &st, PaTile<T, HD> 
 
 // Tiles t0 + wave, t0 + wave + WAVES, .. < t1 of sequence b, K/V head h, query heads h0 .. h0 + gq - 1.  While a tile is
 // worked on the next one of the wave is on its way, and the page numbers of the one behind that.
-template <typename T, int HD, int WAVES>
+template <typename T, int HD, int WAVES, bool ONCE>
 __device__ __forceinline__ void pa_run(const PageAttnArgs &a, int b, int len, int h, int h0, int gq, int t0, int t1, char *lds, PaState<T, HD> &st) {
   using G = PaGeo<T, HD>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
@@ -227,10 +232,10 @@ __device__ __forceinline__ void pa_run(const PageAttnArgs &a, int b, int len, in
     const int kp = __shfl(safe, kr * G::KI, 64), vp = __shfl(safe, g * G::NK, 64);
     const char *p = kh + (int64_t)kp * a.k_page + (int64_t)((key0 + kr * G::KI) & in_page) * a.k_tok;
 #pragma unroll
-    for (int i = 0; i < G::KI; ++i) d.k[i] = ld16_stream(p + i * a.k_tok);
+    for (int i = 0; i < G::KI; ++i) d.k[i] = pa_ld16<ONCE>(p + i * a.k_tok);
     p = vh + (int64_t)vp * a.v_page + (int64_t)((key0 + g * G::NK) & in_page) * a.v_tok;
 #pragma unroll
-    for (int i = 0; i < G::NK; ++i) pa_load_words<G::VW>(d.v[i], p + i * a.v_tok);
+    for (int i = 0; i < G::NK; ++i) pa_load_words<G::VW, ONCE>(d.v[i], p + i * a.v_tok);
   };
   PaTile<T, HD> x, y;
   load(x, t, page_of(next, t));
@@ -318,7 +323,7 @@ __device__ __forceinline__ int pa_len(const PageAttnArgs &a, int b) {
 }
 
 // One workgroup per (sequence, block of query heads): the whole length, no second launch.
-template <typename T, int HD, int WAVES>
+template <typename T, int HD, int WAVES, bool ONCE>
 __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_whole_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
   extern __shared__ __align__(16) char pa_lds[];
@@ -329,7 +334,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_whole_kernel(PageAttn
   const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
   const int len = pa_len(a, b);
   PaState<T, HD> st;
-  pa_run<T, HD, WAVES>(a, b, len, h, h0, gq, 0, (len + PaGeo<T, HD>::TILE - 1) / PaGeo<T, HD>::TILE, own, st);
+  pa_run<T, HD, WAVES, ONCE>(a, b, len, h, h0, gq, 0, (len + PaGeo<T, HD>::TILE - 1) / PaGeo<T, HD>::TILE, own, st);
   pa_join<T, HD, WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, -1);
 }
 
@@ -449,7 +454,7 @@ __device__ __forceinline__ bool pa_find_part(const PageAttnArgs &a, int segs, in
   return out.b >= 0;
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool ONCE>
 __global__ __launch_bounds__(PA_SPLIT_WAVES * 64, 2) void page_attn_split_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
   extern __shared__ __align__(16) char pa_lds[];
@@ -475,7 +480,7 @@ __global__ __launch_bounds__(PA_SPLIT_WAVES * 64, 2) void page_attn_split_kernel
     if (part == 0 && threadIdx.x == 0) a.cuts[1 + found.cut] = int4{b, seg, record, parts};   // (the record of part 0)
   }
   PaState<T, HD> st;
-  pa_run<T, HD, PA_SPLIT_WAVES>(a, b, len, h, h0, gq, t0, t1, own, st);
+  pa_run<T, HD, PA_SPLIT_WAVES, ONCE>(a, b, len, h, h0, gq, t0, t1, own, st);
   pa_join<T, HD, PA_SPLIT_WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, parts > 1 ? record + part : -1);
 }
 
@@ -609,14 +614,16 @@ static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t strea
   const size_t wave_bytes = pa_wave_bytes<T, HD>(rows);
   const unsigned segs = (unsigned)a.batch * (unsigned)(a.kv_heads * a.q_blocks);
   if (whole) {
-    if (rows <= 8 && segs <= PA_WIDE_SEGS) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8>), dim3(segs), dim3(512), 8 * wave_bytes, stream, a);
-    else hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 4>), dim3(segs), dim3(256), 4 * wave_bytes, stream, a);
+    if (rows <= 8 && segs <= PA_WIDE_SEGS) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 8, true>), dim3(segs), dim3(512), 8 * wave_bytes, stream, a);
+    else if (a.q_blocks == 1) hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 4, true>), dim3(segs), dim3(256), 4 * wave_bytes, stream, a);
+    else hipLaunchKernelGGL((page_attn_whole_kernel<T, HD, 4, false>), dim3(segs), dim3(256), 4 * wave_bytes, stream, a);
     return hipGetLastError();
   }
   // parts: as many as a table row's tokens allow, PA_PARTS and one more per segment at most
   const int64_t tile = PaGeo<T, HD>::TILE, longest = ((int64_t)a.room + tile * a.min_tiles - 1) / (tile * a.min_tiles);
   const int64_t all = (int64_t)segs * longest < (int64_t)PA_PARTS + segs ? (int64_t)segs * longest : (int64_t)PA_PARTS + segs;
-  hipLaunchKernelGGL((page_attn_split_kernel<T, HD>), dim3((unsigned)all), dim3(PA_SPLIT_WAVES * 64), PA_SPLIT_WAVES * wave_bytes, stream, a);
+  const auto split = a.q_blocks == 1 ? page_attn_split_kernel<T, HD, true> : page_attn_split_kernel<T, HD, false>;
+  hipLaunchKernelGGL(split, dim3((unsigned)all), dim3(PA_SPLIT_WAVES * 64), PA_SPLIT_WAVES * wave_bytes, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const unsigned cuts = segs < (unsigned)PA_PARTS ? segs : (unsigned)PA_PARTS;
