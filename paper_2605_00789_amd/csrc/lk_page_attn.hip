@@ -34,7 +34,6 @@ struct PageAttnArgs {
   int64_t k_page, k_tok, k_head, v_page, v_tok, v_head, q_tok, q_head, o_tok, o_head;   // bytes
   int batch, kv_heads, group, q_blocks;   // query heads per K/V head, blocks of at most 16 of them
   int n_pages, lg, room;          // room: tokens a table row can hold
-  int min_tiles;                  // split launches: a part has as many tiles, if its segment has
   float scale2;                   // softmax scale * log2(e)
 };
 
@@ -344,7 +343,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void page_attn_whole_kernel(PageAttn
 // loads: lengths, page numbers, rows) while others are in the middle of theirs.  Parts of a segment that is not whole leave
 // records, in the order of their tokens, which a second launch joins.
 constexpr int PA_SPLIT_WAVES = 4, PA_JOIN_THREADS = 256;
+// Parts of a call.  Sequences about as long as each other (the longest at most 3/2 of their mean), or few segments: no more than
+// fit the card, two workgroups of 256 registers a CU.  Otherwise twice as many, so that what is left at the end is small.
+// us a call with 512 / 1024, 8 K/V heads unless named: 131000 tokens 94.3 / 97.6, 16 x 1100 tokens of 32 heads 52.1 / 56.7, 16 x 8192 of 4
+// heads 55.4 / 61.9, 3 x (1 to 8000) of 32 heads 39.6 / 43.0; 64 x (1 to 8192) 193.9 / 176.2, 16 x (50 to 2000) of 32 heads
+// 66.4 / 54.1, 64 x (1 to 4096) 104.4 / 93.5, 24 x (1 to 16000) 134.8 / 128.6.
 constexpr int PA_PARTS = 1024, PA_SLOTS = 512, PA_FEW_SEGS = 192;
+constexpr uint32_t PA_MIN_TILES = PA_SPLIT_WAVES;   // a tile for each wave; 1 x 2048 tokens with 16 / 8 / 4: 13.8 / 12.2 / 10.9 us
 
 // Quotient of numbers that are small in all but impossible calls: a 64-bit division is 130 instructions.
 __device__ __forceinline__ int64_t pa_quotient(int64_t n, int64_t d) {
@@ -401,11 +406,11 @@ __device__ __forceinline__ bool pa_find_part(const PageAttnArgs &a, int segs, in
     // k parts of each segment fit the card at once
     const uint32_t k = n_segs < PA_SLOTS ? PA_SLOTS / (uint32_t)(n_segs ? n_segs : 1) : 1;
     c = ((uint32_t)longest + k - 1) / k;
-    c = c < (uint32_t)a.min_tiles ? a.min_tiles : c;
+    c = c < PA_MIN_TILES ? PA_MIN_TILES : c;
   } else {
     const int target = n_segs < PA_FEW_SEGS ? PA_SLOTS : PA_PARTS;
     const int64_t want = pa_quotient(all_tiles + target - 1, target);
-    c = want < a.min_tiles ? a.min_tiles : (uint32_t)want;
+    c = want < PA_MIN_TILES ? PA_MIN_TILES : (uint32_t)want;
     // rounded up segment by segment they are more than that: longer ones, then
     int n = 0;
     for (int b = b0; b < b1; ++b) n += parts_of(pa_len(a, b), c);
@@ -484,104 +489,86 @@ __global__ __launch_bounds__(PA_SPLIT_WAVES * 64, 2) void page_attn_split_kernel
   pa_join<T, HD, PA_SPLIT_WAVES>(a, pa_lds, wave_bytes, st, b, h0, gq, parts > 1 ? record + part : -1);
 }
 
-// Joins the records of a segment in their order: one workgroup per cut segment, or per query head of it where segments are few
-// and their records many.
+// Joins the records of a cut segment, a workgroup per query head, always in the records' order.
 constexpr int PA_FEW = 4;   // records that a thread loads at once, weights and sums, in one trip to memory
 
-template <typename T, int HD, bool BY_HEAD>
+template <typename T, int HD>
 __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAttnArgs a) {
   fetch_args<PageAttnArgs>();
   extern __shared__ __align__(16) char pa_lds[];
-  __shared__ float tops[PA_MAX_Q], sums[PA_MAX_Q];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ float all_top, all_sum;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int rows = a.group < PA_MAX_Q ? a.group : PA_MAX_Q;
   const int n_cuts = a.cuts[0].x;
   const int4 cut = a.cuts[1 + blockIdx.x];
   if ((int)blockIdx.x >= n_cuts) return;
   const int b = cut.x, seg = cut.y, n_rec = cut.w;
-  const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks;
-  const int gq = a.group - qb * PA_MAX_Q < PA_MAX_Q ? a.group - qb * PA_MAX_Q : PA_MAX_Q, h0 = h * a.group + qb * PA_MAX_Q;
-  const int q0 = BY_HEAD ? blockIdx.y : 0, nq = BY_HEAD ? 1 : gq;
-  if (q0 >= gq) return;
-  constexpr int V = HD / 4;   // four elements a thread
-  const int items = nq * V;
-  auto record = [&](int r) { return (int64_t)(cut.z + r) * rows + q0; };
-  auto finish = [&](int n, int d, float top, float sum, const float4 &o) {
+  const int h = seg / a.q_blocks, qb = seg - h * a.q_blocks, head = h * a.group + qb * PA_MAX_Q + (int)blockIdx.y;
+  if (head >= (h + 1) * a.group) return;   // a block of fewer heads
+  constexpr int V = HD / 4, GROUPS = PA_JOIN_THREADS / V;   // four elements a thread, and every GROUPS-th record
+  const int grp = tid / V, d = (tid - grp * V) * 4;
+  auto record = [&](int r) { return (int64_t)(cut.z + r) * rows + blockIdx.y; };
+  auto weight_of = [](float m, float top) { return m == top ? 1.f : __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top)); };
+  auto finish = [&](float top, float sum, const float4 &o) {
     const float e[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) pa_finish<T>(a, b, h0 + q0 + n, d + k, top, sum, e[k]);
+    for (int k = 0; k < 4; ++k) pa_finish<T>(a, b, head, d + k, top, sum, e[k]);
   };
   if (n_rec <= PA_FEW) {
-    for (int i = tid; i < items; i += PA_JOIN_THREADS) {
-      const int n = i / V, d = (i - n * V) * 4;
-      float2 s[PA_FEW];
-      float4 v[PA_FEW];
+    if (grp != 0) return;
+    float2 s[PA_FEW];
+    float4 v[PA_FEW];
 #pragma unroll
-      for (int r = 0; r < PA_FEW; ++r) {
-        const int64_t k = record(r < n_rec ? r : 0) + n;
-        s[r] = *reinterpret_cast<const float2 *>(a.stats + k * 2);
-        v[r] = *reinterpret_cast<const float4 *>(a.part + k * HD + d);
-      }
-      float top = s[0].x, sum = 0.f;
-#pragma unroll
-      for (int r = 1; r < PA_FEW; ++r) top = fmaxf(top, s[r].x);
-      const float ref = top == -INFINITY ? 0.f : top;
-      float4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int r = 0; r < PA_FEW; ++r) {
-        if (r >= n_rec) continue;
-        const float f = s[r].x == top ? 1.f : __builtin_amdgcn_exp2f(s[r].x - ref);
-        sum += f * s[r].y;
-        o.x += f * v[r].x; o.y += f * v[r].y; o.z += f * v[r].z; o.w += f * v[r].w;
-      }
-      finish(n, d, top, sum, o);
+    for (int r = 0; r < PA_FEW; ++r) {
+      const int64_t k = record(r < n_rec ? r : 0);
+      s[r] = *reinterpret_cast<const float2 *>(a.stats + k * 2);
+      v[r] = *reinterpret_cast<const float4 *>(a.part + k * HD + d);
     }
+    float top = s[0].x, sum = 0.f;
+#pragma unroll
+    for (int r = 1; r < PA_FEW; ++r) top = fmaxf(top, s[r].x);
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < PA_FEW; ++r) {
+      if (r >= n_rec) continue;
+      const float f = weight_of(s[r].x, top);
+      sum += f * s[r].y;
+      o.x += f * v[r].x; o.y += f * v[r].y; o.z += f * v[r].z; o.w += f * v[r].w;
+    }
+    finish(top, sum, o);
     return;
   }
-  float *weight = reinterpret_cast<float *>(pa_lds);    // [nq][n_rec]
-  for (int n = wave; n < nq; n += PA_JOIN_THREADS / 64) {
+  float *weight = reinterpret_cast<float *>(pa_lds);    // [n_rec]
+  if (tid < 64) {
     float top = -INFINITY, sum = 0.f;
-    for (int r = lane; r < n_rec; r += 64) top = fmaxf(top, a.stats[(record(r) + n) * 2]);
+    for (int r = lane; r < n_rec; r += 64) top = fmaxf(top, a.stats[record(r) * 2]);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    const float ref = top == -INFINITY ? 0.f : top;
     for (int r = lane; r < n_rec; r += 64) {
-      const float2 s = *reinterpret_cast<const float2 *>(a.stats + (record(r) + n) * 2);
-      const float f = s.x == top ? 1.f : __builtin_amdgcn_exp2f(s.x - ref);
-      weight[n * n_rec + r] = f;
-      sum += f * s.y;
+      const float2 s = *reinterpret_cast<const float2 *>(a.stats + record(r) * 2);
+      weight[r] = weight_of(s.x, top);
+      sum += weight[r] * s.y;
     }
     sum = wave_sum_butterfly(sum);
-    if (lane == 0) { tops[n] = top; sums[n] = sum; }
+    if (lane == 0) { all_top = top; all_sum = sum; }
   }
   __syncthreads();
-  // where the items are fewer than the threads, groups of threads take every n-th record
-  const int groups = items < PA_JOIN_THREADS ? PA_JOIN_THREADS / items : 1;
-  float4 *part_sum = reinterpret_cast<float4 *>(weight + (((size_t)nq * n_rec + 3) & ~(size_t)3));   // [groups][items]
-  for (int i0 = 0; i0 < items; i0 += PA_JOIN_THREADS) {
-    const int grp = groups > 1 ? tid / items : 0, i = groups > 1 ? tid - grp * items : i0 + tid;
-    const bool mine = grp < groups && i < items;
-    const int n = i / V, d = (i - n * V) * 4;
-    float4 o = {0.f, 0.f, 0.f, 0.f};
-    if (mine) {
+  float4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-      for (int r = grp; r < n_rec; r += groups) {
-        const float4 v = *reinterpret_cast<const float4 *>(a.part + (record(r) + n) * HD + d);
-        const float f = weight[n * n_rec + r];
-        o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
-      }
-    }
-    if (groups > 1) {
-      if (mine) part_sum[grp * items + i] = o;
-      __syncthreads();
-      if (grp != 0) continue;
-      for (int k = 1; k < groups; ++k) {
-        const float4 v = part_sum[k * items + i];
-        o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
-      }
-    }
-    if (mine) finish(n, d, tops[n], sums[n], o);
+  for (int r = grp; r < n_rec; r += GROUPS) {
+    const float4 v = *reinterpret_cast<const float4 *>(a.part + record(r) * HD + d);
+    const float f = weight[r];
+    o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
   }
+  float4 *part_sum = reinterpret_cast<float4 *>(weight + ((n_rec + 3) & ~3));   // [GROUPS][V]
+  part_sum[tid] = o;
+  __syncthreads();
+  if (grp != 0) return;
+  for (int k = 1; k < GROUPS; ++k) {
+    const float4 v = part_sum[k * V + tid];
+    o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+  }
+  finish(all_top, all_sum, o);
 }
 
 // Launches of one workgroup per segment, or split ones?  The host knows a bound on the lengths, not the lengths.  us a call, whole
@@ -596,8 +583,6 @@ constexpr int PA_WHOLE_TOKENS = 768;
 constexpr unsigned PA_WIDE_SEGS = 256;
 constexpr unsigned PA_MANY_SEGS = 160;
 constexpr int PA_WHOLE_TOKENS_MANY = 2048;
-constexpr unsigned PA_JOIN_BY_HEAD = 256;
-constexpr size_t PA_JOIN_WEIGHTS = 8192;   // 32 KB of LDS
 
 // a segment of n parts has more than n - 1 times the tiles of a whole part, and n > 1: at most twice PA_PARTS records, of at most
 // PA_PARTS segments
@@ -620,7 +605,7 @@ static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t strea
     return hipGetLastError();
   }
   // parts: as many as a table row's tokens allow, PA_PARTS and one more per segment at most
-  const int64_t tile = PaGeo<T, HD>::TILE, longest = ((int64_t)a.room + tile * a.min_tiles - 1) / (tile * a.min_tiles);
+  const int64_t tile = PaGeo<T, HD>::TILE, longest = ((int64_t)a.room + tile * PA_MIN_TILES - 1) / (tile * PA_MIN_TILES);
   const int64_t all = (int64_t)segs * longest < (int64_t)PA_PARTS + segs ? (int64_t)segs * longest : (int64_t)PA_PARTS + segs;
   const auto split = a.q_blocks == 1 ? page_attn_split_kernel<T, HD, true> : page_attn_split_kernel<T, HD, false>;
   hipLaunchKernelGGL(split, dim3((unsigned)all), dim3(PA_SPLIT_WAVES * 64), PA_SPLIT_WAVES * wave_bytes, stream, a);
@@ -629,10 +614,8 @@ static hipError_t pa_launch(const PageAttnArgs &a, bool whole, hipStream_t strea
   const unsigned cuts = segs < (unsigned)PA_PARTS ? segs : (unsigned)PA_PARTS;
   // records of a segment: those of a sequence's segments are as many, so PA_PARTS / (their number) + 1 at most
   const size_t most = PA_PARTS / (size_t)(a.kv_heads * a.q_blocks) + 1;
-  const bool by_head = segs < PA_JOIN_BY_HEAD || rows * most > PA_JOIN_WEIGHTS;
-  const size_t join = (((by_head ? 1 : rows) * most + 3) / 4 * 4 + 4 * PA_JOIN_THREADS) * sizeof(float);
-  if (by_head) hipLaunchKernelGGL((page_attn_join_kernel<T, HD, true>), dim3(cuts, rows), dim3(PA_JOIN_THREADS), join, stream, a);
-  else hipLaunchKernelGGL((page_attn_join_kernel<T, HD, false>), dim3(cuts), dim3(PA_JOIN_THREADS), join, stream, a);
+  const size_t join = ((most + 3) / 4 * 4 + 4 * PA_JOIN_THREADS) * sizeof(float);
+  hipLaunchKernelGGL((page_attn_join_kernel<T, HD>), dim3(cuts, rows), dim3(PA_JOIN_THREADS), join, stream, a);
   return hipGetLastError();
 }
 
@@ -697,7 +680,6 @@ lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq
   a.o_tok = p->batch > 1 ? o_tok_stride * eb : 0; a.o_head = p->heads > 1 ? o_head_stride * eb : 0;
   a.batch = p->batch; a.kv_heads = p->kv_heads; a.group = p->heads / p->kv_heads; a.q_blocks = (a.group + PA_MAX_Q - 1) / PA_MAX_Q;
   a.n_pages = p->n_pages; a.lg = log2_of(p->page_tokens); a.room = p->max_pages * p->page_tokens;
-  a.min_tiles = 8;
   a.scale2 = (softmax_scale > 0.f ? softmax_scale : 1.f / sqrtf((float)p->head_dim)) * PA_LOG2E;
   const int bound = max_seq_tokens > 0 && max_seq_tokens < a.room ? max_seq_tokens : a.room;
   const bool whole = bound <= ((unsigned)(a.batch * a.kv_heads * a.q_blocks) < PA_MANY_SEGS ? PA_WHOLE_TOKENS : PA_WHOLE_TOKENS_MANY);
