@@ -543,6 +543,8 @@ lightkv_status lightkv_page_alloc(const lightkv_pages *p, const int32_t *cu_new,
  *   free_pages       [n_pages] in and out: entries from free_count[0] on are written
  *   seq_lens_out     [batch] 0 where done, seq_lens[b] elsewhere.  May be seq_lens itself
  *   free_count_out   [1] may be free_count itself; never more than n_pages (what would not fit the stack is dropped)
+ * A page that several finished sequences hold is put on the stack once for each of them: sequences that share pages (for
+ * lightkv_page_attention they may) must not be given back by this call while others hold theirs.
  */
 lightkv_status lightkv_page_free(const lightkv_pages *p, const int32_t *done, const int32_t *seq_lens, int32_t *free_pages,
                                  const int32_t *free_count, int32_t *seq_lens_out, int32_t *free_count_out, void *stream);
@@ -575,7 +577,9 @@ lightkv_status lightkv_page_attention_workspace(const lightkv_pages *p, size_t *
  *   ws         two calls that share it must be ordered by their streams
  * Scores, softmax and sums are fp32; weights enter the product with bf16 values as the sum of two bf16 numbers.  Where the
  * length is split, the cut depends on the lengths of all sequences of the call, so the last bits of a sequence may differ in
- * another batch; the same call gives the same bits.
+ * another batch; the same call gives the same bits.  Weights below the smallest fp32 number are zero, also against an
+ * infinity.  One launch, or two where the bound lets a sequence be long (more than 768 tokens; 2048 with 160 or more pairs
+ * of a sequence and a K/V head).
  */
 lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq_lens, int32_t max_seq_tokens,
                                       const void *Q, int64_t q_tok_stride, int64_t q_head_stride, float softmax_scale,

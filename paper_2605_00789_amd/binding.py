@@ -384,6 +384,7 @@ PAGED_MAX_BATCH = 4096   # LIGHTKV_PAGED_MAX_BATCH
 # the handle of the current stream: 0.1 us, where making a torch.cuda.Stream for it takes 2.7 of a call's 10
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_I32 = torch.int32
 _PAGE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
@@ -428,30 +429,32 @@ class Pages:
 
     def _ints(self, t, n, what):
         """An int32 array of at least n entries on the cache's device."""
-        if t.dtype is torch.int32 and t.get_device() == self.index and t.numel() >= n and t.is_contiguous():
+        if t.dtype is _I32 and t.get_device() == self.index and t.numel() >= n and t.is_contiguous():
             return t.data_ptr()
         raise ValueError("%s: contiguous int32 of at least %d entries on the table's device" % (what, n))
 
     def _rows(self, t, heads, n, what):
         """Rows [n or more, heads, head_dim] (or [.., heads * head_dim]): pointer and strides."""
-        if t.dtype is not self.dtype or t.get_device() != self.index:
-            raise ValueError("%s: %s on the table's device" % (what, self.dtype))
-        shape, stride, d = t.shape, t.stride(), self.head_dim
-        if len(shape) == 3:
-            if shape[1] == heads and shape[2] == d and stride[2] == 1 and shape[0] >= n:
-                return t.data_ptr(), stride[0], stride[1]
-        elif len(shape) == 2 and shape[1] == heads * d and stride[1] == 1 and shape[0] >= n:
-            return t.data_ptr(), stride[0], d
-        raise ValueError("%s: [%d or more, %d, %d] with contiguous elements" % (what, n, heads, d))
+        d, shape = self.head_dim, t.shape
+        if t.dtype is self.dtype and t.get_device() == self.index and shape[0] >= n:
+            flat = len(shape) == 2 and shape[1] == heads * d
+            if flat or (len(shape) == 3 and shape[1] == heads and shape[2] == d):
+                if t.is_contiguous():
+                    return t.data_ptr(), heads * d, d
+                stride = t.stride()
+                if stride[-1] == 1:
+                    return t.data_ptr(), stride[0], d if flat else stride[1]
+        raise ValueError("%s: %s [%d or more, %d, %d] with contiguous elements on the table's device" % (what, self.dtype, n, heads, d))
 
     def _call(self, fn, where, args, stream):
         """The call on its stream: that of the cache's device, with this device current."""
+        s = _raw_stream(self.index) if stream is None else stream.cuda_stream
         if _current_device() == self.index:
-            st = fn(self._ref, *args, _raw_stream(self.index) if stream is None else stream.cuda_stream)
+            st = fn(self._ref, *args, s)
         else:
             with torch.cuda.device(self.device):
-                st = fn(self._ref, *args, _raw_stream(self.index) if stream is None else stream.cuda_stream)
-        if st != 0:
+                st = fn(self._ref, *args, s)
+        if st:
             raise LightKVError(st, where)
 
 
@@ -477,9 +480,13 @@ def lightkv_page_free(p: Pages, done, seq_lens, free_pages, free_count, seq_lens
 
 
 def lightkv_page_write(p: Pages, slots, K, V, *, cu_new=None, stream=None):
-    """Rows K, V [rows, kv_heads, head_dim] (or [rows, kv_heads * head_dim]) into their slots; with cu_new only the first
-    cu_new[batch] of them.  K or V may be None."""
-    rows = min(t.shape[0] for t in (K, V, slots) if t is not None)
+    """Rows K, V [rows, kv_heads, head_dim] (or [rows, kv_heads * head_dim]) into their slots, as many as the shortest of the
+    three has; with cu_new only the first cu_new[batch] of them.  K or V may be None."""
+    rows = slots.numel()
+    if K is not None:
+        rows = min(rows, K.shape[0])
+    if V is not None:
+        rows = min(rows, V.shape[0])
     if rows == 0:
         return
     h = p.kv_heads

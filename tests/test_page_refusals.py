@@ -164,3 +164,13 @@ def test_binding_refuses_host_tensors(B):
         B.Pages(torch.zeros(2, 2, dtype=torch.int32), n_pages=4, page_tokens=16)
     with pytest.raises(ValueError):
         B.Pages(torch.zeros(2, 2), n_pages=4, page_tokens=16)
+
+
+def test_no_page_kernel_keeps_anything_in_scratch_memory(B):
+    """Tiles on their way are what these kernels' rate rests on: a load that is parked in scratch memory is waited for first."""
+    from test_code_objects import _kernels
+    kernels = {k: m for k, m in _kernels(B.lib_path()).items() if "page_" in k}
+    for name in ("page_alloc", "page_free", "page_write", "page_attn_whole", "page_attn_split", "page_attn_join"):
+        assert any(name in k for k in kernels), name
+    scratch = {k: m[".private_segment_fixed_size"] for k, m in kernels.items() if m[".private_segment_fixed_size"]}
+    assert not scratch, scratch
