@@ -380,11 +380,17 @@ def lightkv_compress_schedule_ratio(stages: StageArray, rho, tiles, grid_h, grid
 
 
 # ---- paged cache ------------------------------------------------------------------------------------------------------
+# These calls are made once a layer and token: their tensors are checked and handed on by a module of host code beside the
+# library (csrc/lk_pages_torch.cpp) -- 3 us of Python a call, otherwise, beside a launch of as many.
+try:
+    from . import _lk_pages
+except ImportError as e:
+    raise ImportError("_lk_pages.so is not built or does not load (%s). Run `python paper_2605_00789_amd/build.py`." % e) from e
+
 PAGED_MAX_BATCH = 4096   # LIGHTKV_PAGED_MAX_BATCH
-# the handle of the current stream: 0.1 us, where making a torch.cuda.Stream for it takes 2.7 of a call's 10
+# the handle of the current stream: 0.1 us, where making a torch.cuda.Stream for it takes 2.7
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-_I32 = torch.int32
 _PAGE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
@@ -423,77 +429,40 @@ class Pages:
         else:
             c.n_pages, c.page_tokens = int(n_pages), int(page_tokens)
         self._ref = C.byref(c)
-        # what every call looks at, without a trip through ctypes or a torch.device (a call's host time is its cost for few rows)
-        self.index, self.batch, self.heads, self.kv_heads, self.head_dim = self.device.index, c.batch, c.heads, c.kv_heads, c.head_dim
-        self.n_pages = c.n_pages
+        self._at, self.index = C.addressof(c), self.device.index
 
-    def _ints(self, t, n, what):
-        """An int32 array of at least n entries on the cache's device."""
-        if t.dtype is _I32 and t.get_device() == self.index and t.numel() >= n and t.is_contiguous():
-            return t.data_ptr()
-        raise ValueError("%s: contiguous int32 of at least %d entries on the table's device" % (what, n))
 
-    def _rows(self, t, heads, n, what):
-        """Rows [n or more, heads, head_dim] (or [.., heads * head_dim]): pointer and strides."""
-        d, shape = self.head_dim, t.shape
-        if t.dtype is self.dtype and t.get_device() == self.index and shape[0] >= n:
-            flat = len(shape) == 2 and shape[1] == heads * d
-            if flat or (len(shape) == 3 and shape[1] == heads and shape[2] == d):
-                if t.is_contiguous():
-                    return t.data_ptr(), heads * d, d
-                stride = t.stride()
-                if stride[-1] == 1:
-                    return t.data_ptr(), stride[0], d if flat else stride[1]
-        raise ValueError("%s: %s [%d or more, %d, %d] with contiguous elements on the table's device" % (what, self.dtype, n, heads, d))
-
-    def _call(self, fn, where, args, stream):
-        """The call on its stream: that of the cache's device, with this device current."""
-        s = _raw_stream(self.index) if stream is None else stream.cuda_stream
-        if _current_device() == self.index:
-            st = fn(self._ref, *args, s)
-        else:
-            with torch.cuda.device(self.device):
-                st = fn(self._ref, *args, s)
-        if st:
-            raise LightKVError(st, where)
+def _page_call(fn, where, p, args, stream):
+    """The call on its stream: that of the cache's device, with this device current."""
+    index = p.index
+    s = _raw_stream(index) if stream is None else stream.cuda_stream
+    if _current_device() == index:
+        st = fn(p._at, index, *args, s)
+    else:
+        with torch.cuda.device(index):
+            st = fn(p._at, index, *args, s)
+    if st:
+        raise LightKVError(st, where)
 
 
 def lightkv_page_alloc(p: Pages, cu_new, seq_lens, free_pages, free_count, seq_lens_out, free_count_out, slots, *,
                        status=None, stream=None):
     """Pages and slots for cu_new[b + 1] - cu_new[b] more tokens of every sequence; seq_lens_out and free_count_out may be
-    seq_lens and free_count themselves."""
-    n, ints = p.batch, p._ints
-    args = (ints(cu_new, n + 1, "cu_new"), ints(seq_lens, n, "seq_lens"), ints(free_pages, p.n_pages, "free_pages"),
-            ints(free_count, 1, "free_count"), ints(seq_lens_out, n, "seq_lens_out"),
-            ints(free_count_out, 1, "free_count_out"), ints(slots, 0, "slots"), slots.numel(),
-            None if status is None else ints(status, n, "status"))
-    p._call(_lib.lightkv_page_alloc, "lightkv_page_alloc", args, stream)
+    seq_lens and free_count themselves.  All arrays int32."""
+    _page_call(_lk_pages.page_alloc, "lightkv_page_alloc", p,
+               (cu_new, seq_lens, free_pages, free_count, seq_lens_out, free_count_out, slots, status), stream)
 
 
 def lightkv_page_free(p: Pages, done, seq_lens, free_pages, free_count, seq_lens_out, free_count_out, *, stream=None):
-    """Pages of every sequence with done[b] != 0 back onto the stack."""
-    n, ints = p.batch, p._ints
-    args = (ints(done, n, "done"), ints(seq_lens, n, "seq_lens"), ints(free_pages, p.n_pages, "free_pages"),
-            ints(free_count, 1, "free_count"), ints(seq_lens_out, n, "seq_lens_out"),
-            ints(free_count_out, 1, "free_count_out"))
-    p._call(_lib.lightkv_page_free, "lightkv_page_free", args, stream)
+    """Pages of every sequence with done[b] != 0 back onto the stack.  All arrays int32."""
+    _page_call(_lk_pages.page_free, "lightkv_page_free", p,
+               (done, seq_lens, free_pages, free_count, seq_lens_out, free_count_out), stream)
 
 
 def lightkv_page_write(p: Pages, slots, K, V, *, cu_new=None, stream=None):
     """Rows K, V [rows, kv_heads, head_dim] (or [rows, kv_heads * head_dim]) into their slots, as many as the shortest of the
     three has; with cu_new only the first cu_new[batch] of them.  K or V may be None."""
-    rows = slots.numel()
-    if K is not None:
-        rows = min(rows, K.shape[0])
-    if V is not None:
-        rows = min(rows, V.shape[0])
-    if rows == 0:
-        return
-    h = p.kv_heads
-    k = (None, 0, 0) if K is None else p._rows(K, h, rows, "K")
-    v = (None, 0, 0) if V is None else p._rows(V, h, rows, "V")
-    args = (None if cu_new is None else p._ints(cu_new, p.batch + 1, "cu_new"), p._ints(slots, rows, "slots"), rows, *k, *v)
-    p._call(_lib.lightkv_page_write, "lightkv_page_write", args, stream)
+    _page_call(_lk_pages.page_write, "lightkv_page_write", p, (slots, K, V, cu_new), stream)
 
 
 def lightkv_page_attention_workspace(p: Pages) -> int:
@@ -505,12 +474,5 @@ def lightkv_page_attention_workspace(p: Pages) -> int:
 def lightkv_page_attention(p: Pages, seq_lens, Q, out, ws, *, lse=None, softmax_scale=0.0, max_seq_tokens=0, stream=None):
     """Attention of one new token per sequence: Q, out [batch, heads, head_dim] (or [batch, heads * head_dim]); lse: optional
     fp32 [heads, batch]; ws: uint8 of lightkv_page_attention_workspace(p) bytes."""
-    n, heads = p.batch, p.heads
-    if lse is not None and (lse.dtype is not torch.float32 or lse.get_device() != p.index or lse.numel() < heads * n or not lse.is_contiguous()):
-        raise ValueError("lse: contiguous float32 [heads, batch] on the table's device")
-    if ws.get_device() != p.index or not ws.is_contiguous():
-        raise ValueError("ws: contiguous memory on the table's device")
-    args = (p._ints(seq_lens, n, "seq_lens"), int(max_seq_tokens), *p._rows(Q, heads, n, "Q"), float(softmax_scale),
-            *p._rows(out, heads, n, "out"), None if lse is None else lse.data_ptr(), ws.data_ptr(),
-            ws.nbytes)
-    p._call(_lib.lightkv_page_attention, "lightkv_page_attention", args, stream)
+    _page_call(_lk_pages.page_attention, "lightkv_page_attention", p,
+               (seq_lens, Q, out, ws, lse, softmax_scale, max_seq_tokens), stream)

@@ -174,3 +174,17 @@ def test_no_page_kernel_keeps_anything_in_scratch_memory(B):
         assert any(name in k for k in kernels), name
     scratch = {k: m[".private_segment_fixed_size"] for k, m in kernels.items() if m[".private_segment_fixed_size"]}
     assert not scratch, scratch
+
+
+def test_calls_refuse_what_is_no_tensor_of_the_cache(B):
+    """What the module behind the calls makes of wrong arguments: a ValueError that names the argument, before anything is launched."""
+    import torch
+    ext, p = B._lk_pages, _pages(B)
+    at_p, host, i = C.addressof(p), torch.zeros(3, 8, 64, dtype=torch.bfloat16), torch.zeros(64, dtype=torch.int32)
+    for name, call in (("cu_new", lambda: ext.page_alloc(at_p, 0, i, i, i, i, i, i, i, None, 0)), ("done", lambda: ext.page_free(at_p, 0, None, i, i, i, i, i, 0)),
+                       ("slots", lambda: ext.page_write(at_p, 0, i, host, host, None, 0)), ("seq_lens", lambda: ext.page_attention(at_p, 0, 3.5, host, host, host, None, 0.0, 0, 0)),
+                       ("arguments", lambda: ext.page_attention(at_p, 0)), ("arguments", lambda: ext.page_alloc()), ("cu_new", lambda: ext.page_alloc(at_p, 0, *[None] * 9))):
+        with pytest.raises(ValueError, match=name):
+            call()
+    with pytest.raises((ValueError, TypeError)):
+        ext.page_free("x", 0, i, i, i, i, i, i, 0)
