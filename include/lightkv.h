@@ -502,7 +502,7 @@ typedef struct lightkv_pages {
   int32_t batch;              /* sequences, = rows of the table; 1 .. LIGHTKV_PAGED_MAX_BATCH                   */
   int32_t n_pages;            /* pages of the pool; n_pages * page_tokens < 2^31                                */
   int32_t page_tokens;        /* rows of a page: a power of two from 8 to 1024                                  */
-  int32_t max_pages;          /* entries of a table row; max_pages * page_tokens < 2^31                         */
+  int32_t max_pages;          /* entries of a table row; max_pages * page_tokens <= 2^30                        */
   int64_t table_stride;       /* ints from one row of the table to the next, >= max_pages                       */
   int32_t *table;             /* device                                                                         */
   /* the rest is used by lightkv_page_write and lightkv_page_attention only                                     */
@@ -551,8 +551,8 @@ lightkv_status lightkv_page_free(const lightkv_pages *p, const int32_t *done, co
 
 /*
  * Rows into their slots: row t of K and V (element e of head h at K[t*k_tok_stride + h*k_head_stride + e]) becomes row
- * slots[t] % page_tokens of page slots[t] / page_tokens of the pools.  Rows t < min(rows, cu_new[batch]) are looked at (all
- * `rows` if cu_new is NULL); a slot that is negative or behind the pool's last page leaves its row out.  K or V may be NULL
+ * slots[t] % page_tokens of page slots[t] / page_tokens of the pools.  Rows cu_new[0] <= t < min(rows, cu_new[batch]) are looked
+ * at (all `rows` if cu_new is NULL); a slot that is negative or behind the pool's last page leaves its row out.  K or V may be NULL
  * (skipped).  Slots should differ: of two rows with one slot, either may be found there afterwards, in parts too.
  * The rows must not overlap the pools.
  */

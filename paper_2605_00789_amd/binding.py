@@ -461,7 +461,7 @@ def lightkv_page_free(p: Pages, done, seq_lens, free_pages, free_count, seq_lens
 
 def lightkv_page_write(p: Pages, slots, K, V, *, cu_new=None, stream=None):
     """Rows K, V [rows, kv_heads, head_dim] (or [rows, kv_heads * head_dim]) into their slots, as many as the shortest of the
-    three has; with cu_new only the first cu_new[batch] of them.  K or V may be None."""
+    three has; with cu_new only rows cu_new[0] to cu_new[batch].  K or V may be None."""
     _page_call(_lk_pages.page_write, "lightkv_page_write", p, (slots, K, V, cu_new), stream)
 
 

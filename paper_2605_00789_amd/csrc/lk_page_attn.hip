@@ -662,12 +662,18 @@ lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq
   st = check_strided(Q, eb, q_tok_stride, p->batch, q_head_stride, p->heads);
   if (st == LIGHTKV_OK) st = check_strided(out, eb, o_tok_stride, p->batch, o_head_stride, p->heads);
   if (st != LIGHTKV_OK) return st;
-  const uint64_t out_bytes = strided_bytes(eb, o_tok_stride, p->batch, o_head_stride, p->heads, p->head_dim);
-  const uint64_t lse_bytes = lse ? (uint64_t)p->heads * p->batch * 4 : 0, len_bytes = (uint64_t)p->batch * 4;
-  if (overlap(Q, strided_bytes(eb, q_tok_stride, p->batch, q_head_stride, p->heads, p->head_dim), out, out_bytes)) return LIGHTKV_ERR_SHAPE;
-  if (overlap(lse, lse_bytes, out, out_bytes) || overlap(seq_lens, len_bytes, out, out_bytes) || overlap(seq_lens, len_bytes, lse, lse_bytes)) return LIGHTKV_ERR_SHAPE;
-  const uint64_t k_bytes = pool_bytes(p, p->k_page_stride, p->k_tok_stride, p->k_head_stride), v_bytes = pool_bytes(p, p->v_page_stride, p->v_tok_stride, p->v_head_stride);
-  if (overlap(p->K, k_bytes, out, out_bytes) || overlap(p->V, v_bytes, out, out_bytes) || overlap(ws, ws_bytes, out, out_bytes)) return LIGHTKV_ERR_SHAPE;
+  // nothing that is written may lie in what is read, or in each other
+  struct Range { const void *at; uint64_t bytes; };
+  const Range in[] = {{Q, strided_bytes(eb, q_tok_stride, p->batch, q_head_stride, p->heads, p->head_dim)}, {seq_lens, (uint64_t)p->batch * 4},
+                      {p->table, ((uint64_t)p->table_stride * (p->batch - 1) + p->max_pages) * 4},
+                      {p->K, pool_bytes(p, p->k_page_stride, p->k_tok_stride, p->k_head_stride)}, {p->V, pool_bytes(p, p->v_page_stride, p->v_tok_stride, p->v_head_stride)}};
+  const Range written[] = {{out, strided_bytes(eb, o_tok_stride, p->batch, o_head_stride, p->heads, p->head_dim)}, {lse, (uint64_t)p->heads * p->batch * 4}, {ws, pa_bytes(p)}};
+  for (int i = 0; i < 3; ++i) {
+    for (const Range &r : in)
+      if (overlap(r.at, r.bytes, written[i].at, written[i].bytes)) return LIGHTKV_ERR_SHAPE;
+    for (int j = 0; j < i; ++j)
+      if (overlap(written[j].at, written[j].bytes, written[i].at, written[i].bytes)) return LIGHTKV_ERR_SHAPE;
+  }
   // rows of the output must not share elements
   const int64_t o_stride[2] = {o_tok_stride, o_head_stride}, o_count[2] = {p->batch, p->heads};
   if (!apart(p->head_dim, o_stride, o_count, 2)) return LIGHTKV_ERR_SHAPE;

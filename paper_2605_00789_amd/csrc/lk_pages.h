@@ -9,6 +9,7 @@
 namespace lk {
 
 constexpr int PAGE_MIN_TOKENS = 8, PAGE_MAX_TOKENS = 1024;
+constexpr int64_t PAGE_MAX_SEQ = 1ll << 30;   // tokens of a table row: positions and a tile or page beyond them are ints
 
 inline bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 inline bool ints_ok(const void *p) { return p && aligned_to(p, 4); }
@@ -20,7 +21,7 @@ inline lightkv_status check_page_table(const lightkv_pages *p) {
   if (p->batch < 1 || p->n_pages < 1 || p->max_pages < 1 || p->page_tokens < 1 || p->table_stride < p->max_pages) return LIGHTKV_ERR_SHAPE;
   if (!aligned_to(p->table, 4) || p->batch > LIGHTKV_PAGED_MAX_BATCH) return LIGHTKV_ERR_UNSUPPORTED;
   if (p->page_tokens < PAGE_MIN_TOKENS || p->page_tokens > PAGE_MAX_TOKENS || (p->page_tokens & (p->page_tokens - 1))) return LIGHTKV_ERR_UNSUPPORTED;
-  if ((int64_t)p->n_pages * p->page_tokens >= (1ll << 31) || (int64_t)p->max_pages * p->page_tokens >= (1ll << 31)) return LIGHTKV_ERR_UNSUPPORTED;
+  if ((int64_t)p->n_pages * p->page_tokens >= (1ll << 31) || (int64_t)p->max_pages * p->page_tokens > PAGE_MAX_SEQ) return LIGHTKV_ERR_UNSUPPORTED;
   return LIGHTKV_OK;
 }
 

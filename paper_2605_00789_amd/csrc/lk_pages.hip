@@ -232,7 +232,12 @@ __global__ __launch_bounds__(PG_THREADS) void page_write_kernel(WriteArgs g) {
   fetch_args<WriteArgs>();
   const int y = blockIdx.y;
   int64_t rows = g.rows;
-  if (g.cu_new) { const int n = g.cu_new[g.batch]; rows = n < rows ? n : rows; }
+  int begin = 0;
+  if (g.cu_new) {
+    const int n = g.cu_new[g.batch];
+    rows = n < rows ? n : rows;
+    begin = g.cu_new[0];
+  }
   const int per = g.pieces_per_row, in_head = (1 << g.lg_pieces) - 1;
   for (int64_t r0 = (int64_t)blockIdx.x * g.rows_per_wg; r0 < rows; r0 += (int64_t)gridDim.x * g.rows_per_wg) {
     const int n_rows = rows - r0 < g.rows_per_wg ? (int)(rows - r0) : g.rows_per_wg;
@@ -246,7 +251,7 @@ __global__ __launch_bounds__(PG_THREADS) void page_write_kernel(WriteArgs g) {
         head[u] = k >> g.lg_pieces;
         piece[u] = (k & in_head) * 16;
         slot[u] = -1;
-        if (i < n_rows * per) slot[u] = g.slots[r0 + r];
+        if (i < n_rows * per && r0 + r >= begin) slot[u] = g.slots[r0 + r];
         v[u] = uint4{0u, 0u, 0u, 0u};
         const char *from = g.src[y] + (r0 + r) * g.src_tok[y] + head[u] * g.src_head[y] + piece[u];
         if (i < n_rows * per) v[u] = STREAM ? ld16_stream(from) : ld16(from);

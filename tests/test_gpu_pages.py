@@ -196,6 +196,21 @@ def test_rows_into_pages(dtype, H, D, P, layout, rows):
             K.copy_(pool(n_pages, P, H, D, dt, layout, seed=1)), V.copy_(pool(n_pages, P, H, D, dt, layout, seed=2))
 
 
+def test_rows_in_front_of_the_first_sequence_stay_out():
+    """Offsets that begin behind row 0: the slots in front are of an earlier call and still name other tokens' places."""
+    from paper_2605_00789_amd import binding as B
+    K, V = (pool(4, 8, 2, 32, torch.float32, "head", fill=1.0) for _ in range(2))
+    pages = B.Pages(torch.zeros(2, 2, **I32), K=K, V=V, heads=2)
+    rows = torch.full((9, 2, 32), 5.0, device=DEV)
+    B.lightkv_page_write(pages, ints(list(range(9))), rows, rows, cu_new=ints([4, 5, 7]))
+    want = torch.ones(4, 8, 2, 32, device=DEV)
+    want[0, 4:7] = 5.0
+    assert torch.equal(K, want) and torch.equal(V, want)
+    B.lightkv_page_write(pages, ints(list(range(9))), rows * 2, rows, cu_new=ints([-3, 0, 1]))
+    want[0, 0] = 10.0
+    assert torch.equal(K, want)
+
+
 # ---- attention --------------------------------------------------------------------------------------------------------
 def scattered(lens, P, n_pages, width, seed):
     """A table whose pages lie anywhere in the pool; entries behind a sequence's last page are stale."""

@@ -33,6 +33,7 @@ TABLE = [
     (dict(table_stride=3), SHAPE), (dict(table=at(0) + 2), UNSUPPORTED), (dict(batch=4097), UNSUPPORTED),
     (dict(page_tokens=4), UNSUPPORTED), (dict(page_tokens=24), UNSUPPORTED), (dict(page_tokens=2048), UNSUPPORTED),
     (dict(n_pages=1 << 27, page_tokens=16), UNSUPPORTED), (dict(max_pages=1 << 27, table_stride=1 << 27), UNSUPPORTED),
+    (dict(max_pages=(1 << 26) + 1, table_stride=1 << 27), UNSUPPORTED),
 ]
 POOLS = TABLE + [
     (dict(kv_heads=0), SHAPE), (dict(heads=0), SHAPE), (dict(heads=7), SHAPE), (dict(head_dim=48), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED),
@@ -62,7 +63,7 @@ def _write(B, p, **o):
 
 
 def _attend(B, p, **o):
-    a = dict(lens=at(3), bound=0, Q=at(4), qt=512, qh=64, scale=0.0, out=at(5), ot=512, oh=64, lse=at(6), ws=at(7), bytes=1 << 30)
+    a = dict(lens=at(3), bound=0, Q=at(4), qt=512, qh=64, scale=0.0, out=at(5), ot=512, oh=64, lse=at(6), ws=at(7), bytes=1 << 24)
     a.update(o)
     return B._lib.lightkv_page_attention(C.byref(p) if p is not None else None, a["lens"], a["bound"], a["Q"], a["qt"], a["qh"], a["scale"], a["out"],
                                          a["ot"], a["oh"], a["lse"], a["ws"], a["bytes"], None)
@@ -149,11 +150,14 @@ def test_attention_arguments(B):
     assert _attend(B, p, Q=at(4) + 8) == UNSUPPORTED and _attend(B, p, qt=509) == UNSUPPORTED and _attend(B, p, oh=68) == UNSUPPORTED
     assert _attend(B, p, lens=at(3) + 2) == UNSUPPORTED and _attend(B, p, lse=at(6) + 2) == UNSUPPORTED
     assert _attend(B, p, out=at(4)) == SHAPE and _attend(B, p, out=at(4) + 512) == SHAPE and _attend(B, p, lse=at(5) + 64) == SHAPE
+    assert _attend(B, p, out=at(1)) == SHAPE and _attend(B, p, out=at(2) + 16) == SHAPE and _attend(B, p, ws=at(4)) == SHAPE and _attend(B, p, lse=at(0)) == SHAPE
+    assert _attend(B, p, ws=at(0)) == SHAPE and _attend(B, p, lse=at(7) + 512) == SHAPE and _attend(B, p, ws=at(1)) == SHAPE and _attend(B, p, lse=at(2)) == SHAPE
     assert _attend(B, p, oh=32) == SHAPE and _attend(B, p, ot=0) == SHAPE              # rows of the output in each other
     n = C.c_size_t(0)
     assert B._lib.lightkv_page_attention_workspace(C.byref(p), C.byref(n)) == OK and n.value > 0
     assert _attend(B, p, ws=None) == WORKSPACE and _attend(B, p, ws=at(7) + 16) == WORKSPACE and _attend(B, p, bytes=n.value - 1) == WORKSPACE
-    # tiles of all rows of the table are counted in 32 bits
+    # 2^30 tokens in a row are the most; tiles of all rows of the table are counted in 32 bits
+    assert _attend(B, _pages(B, max_pages=1 << 26, table_stride=1 << 26), ws=None) == WORKSPACE
     wide = _pages(B, batch=4096, max_pages=1 << 24, table_stride=1 << 24)
     assert _attend(B, wide) == UNSUPPORTED
 
