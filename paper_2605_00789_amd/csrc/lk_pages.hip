@@ -8,14 +8,17 @@
 // workgroup, in LDS: one trip to memory and one scan, where a launch that leaves it in memory for a second one would cost
 // the second launch and the same trip.  A page that is handed out begins with a new token, so the thread that makes that token's
 // slot also writes the table entry and nothing has to be scattered separately.  The time is that chain -- lengths, sum, search,
-// page, store -- 3.7 us behind the launch for a token each of 64 sequences, 8 for 1.8 M slots (7 MB).
+// page, store -- 4.2 us with the launch for a token each of 64 sequences, 9.9 for 1.8 M slots (7 MB).
 #include "lk_common.h"
 #include "lk_pages.h"
 
 namespace lk {
 
 constexpr int PG_THREADS = 256;
-constexpr int PG_SLOTS_PER_THREAD = 4;     // one 16-byte store
+constexpr int PG_SLOTS_PER_THREAD = 4;     // one 16-byte store, mostly one page to look up
+// Up to so many, one workgroup and a slot a thread: decoded tokens have a page each to look up.  us, a slot / four slots a thread: 64
+// sequences of a token 4.2 / 6.2, 256 4.5 / 6.5, 4 of 100 tokens 4.6 / 5.3; 8 of 120 6.2 / 5.5, 1000 of a token 9.8 / 8.2.
+constexpr int PG_FEW_SLOTS = 512;
 // Workgroups of a launch at most: each takes the running sum again, and fewer leave the slots to too few waves.  1.8 M slots of 700
 // sequences with 512 / 1024 / 1536: 14.8 / 10.6 / 9.9 us, 1.25 M of 1000 13.3 / 10.9 / 9.6.
 constexpr int PG_MAX_WGS = 1536;
@@ -76,6 +79,7 @@ __device__ __forceinline__ int clamped_count(const int32_t *count, int n_pages) 
 }
 
 // LDS: cu [batch + 1], length [batch], queue place [batch] (-1: refused)
+template <int SLOTS>
 __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
   fetch_args<AllocArgs>();
   extern __shared__ int pg_lds[];
@@ -124,14 +128,14 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
   }
   if (!(g.what & 1)) return;
   const int64_t end = cu[g.batch] < g.slot_rows ? cu[g.batch] : g.slot_rows;
-  const int64_t step = (int64_t)gridDim.x * PG_THREADS * PG_SLOTS_PER_THREAD;
+  const int64_t step = (int64_t)gridDim.x * PG_THREADS * SLOTS;
   const bool wide = (reinterpret_cast<uintptr_t>(g.slots) & 15) == 0;
-  for (int64_t t0 = ((int64_t)blockIdx.x * PG_THREADS + tid) * PG_SLOTS_PER_THREAD; t0 < end; t0 += step) {
-    int b = 0, page = -1, page_j = -1, page_b = -1, out[PG_SLOTS_PER_THREAD];
+  for (int64_t t0 = ((int64_t)blockIdx.x * PG_THREADS + tid) * SLOTS; t0 < end; t0 += step) {
+    int b = 0, page = -1, page_j = -1, page_b = -1, out[SLOTS];
     unsigned have = 0;
     if (cu[0] <= t0) b = last_not_above(cu, g.batch, (int)t0);
 #pragma unroll
-    for (int i = 0; i < PG_SLOTS_PER_THREAD; ++i) {
+    for (int i = 0; i < SLOTS; ++i) {
       const int64_t t = t0 + i;
       out[i] = -1;
       if (t >= end) continue;
@@ -148,11 +152,11 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
       if (j >= old && (pos & (P - 1)) == 0) g.table[(int64_t)b * g.table_stride + j] = page;
       if ((unsigned)page < (unsigned)g.n_pages) out[i] = (page << g.lg) + (pos & (P - 1));
     }
-    if (wide && have == (1u << PG_SLOTS_PER_THREAD) - 1) {
-      *reinterpret_cast<int4 *>(g.slots + t0) = int4{out[0], out[1], out[2], out[3]};
+    if (SLOTS == 4 && wide && have == (1u << SLOTS) - 1) {
+      *reinterpret_cast<int4 *>(g.slots + t0) = int4{out[0], out[1 % SLOTS], out[2 % SLOTS], out[3 % SLOTS]};
     } else {
 #pragma unroll
-      for (int i = 0; i < PG_SLOTS_PER_THREAD; ++i)
+      for (int i = 0; i < SLOTS; ++i)
         if (have & (1u << i)) g.slots[t0 + i] = out[i];
     }
   }
@@ -303,16 +307,17 @@ lightkv_status lightkv_page_alloc(const lightkv_pages *p, const int32_t *cu_new,
   g.table_stride = p->table_stride; g.slot_rows = slot_rows; g.batch = p->batch; g.max_pages = p->max_pages;
   g.n_pages = p->n_pages; g.lg = log2_of(p->page_tokens);
   const size_t lds = (3 * (size_t)p->batch + 1) * sizeof(int);
-  const int64_t per_wg = PG_THREADS * PG_SLOTS_PER_THREAD, want = (slot_rows + per_wg - 1) / per_wg;
+  const bool few = slot_rows <= PG_FEW_SLOTS;
+  const int64_t per_wg = PG_THREADS * PG_SLOTS_PER_THREAD, want = few ? 1 : (slot_rows + per_wg - 1) / per_wg;
   const int wgs = (int)(want < 1 ? 1 : (want > PG_MAX_WGS ? PG_MAX_WGS : want));
   // lengths and count may be written in place: then only behind the workgroups that still read them
   const bool in_place = seq_lens_out == seq_lens || free_count_out == free_count;
   g.what = wgs > 1 && in_place ? 1 : 3;
-  hipLaunchKernelGGL(page_alloc_kernel, dim3(wgs), dim3(PG_THREADS), lds, static_cast<hipStream_t>(stream), g);
+  hipLaunchKernelGGL(few ? page_alloc_kernel<1> : page_alloc_kernel<PG_SLOTS_PER_THREAD>, dim3(wgs), dim3(PG_THREADS), lds, static_cast<hipStream_t>(stream), g);
   if (g.what == 1) {
     if (hipGetLastError() != hipSuccess) return LIGHTKV_ERR_LAUNCH;
     g.what = 2;
-    hipLaunchKernelGGL(page_alloc_kernel, dim3(1), dim3(PG_THREADS), lds, static_cast<hipStream_t>(stream), g);
+    hipLaunchKernelGGL(page_alloc_kernel<PG_SLOTS_PER_THREAD>, dim3(1), dim3(PG_THREADS), lds, static_cast<hipStream_t>(stream), g);
   }
   return hipGetLastError() == hipSuccess ? LIGHTKV_OK : LIGHTKV_ERR_LAUNCH;
 }
