@@ -354,7 +354,10 @@ constexpr int PA_SPLIT_WAVES = 4, PA_JOIN_THREADS = 256;
 // us a call with 512 / 1024, 8 K/V heads unless named: 131000 tokens 94.3 / 97.6, 16 x 1100 tokens of 32 heads 52.1 / 56.7, 16 x 8192 of 4
 // heads 55.4 / 61.9, 3 x (1 to 8000) of 32 heads 39.6 / 43.0; 64 x (1 to 8192) 193.9 / 176.2, 16 x (50 to 2000) of 32 heads
 // 66.4 / 54.1, 64 x (1 to 4096) 104.4 / 93.5, 24 x (1 to 16000) 134.8 / 128.6.
-constexpr int PA_PARTS = 1024, PA_SLOTS = 512, PA_FEW_SEGS = 192;
+constexpr int PA_PARTS = 1024, PA_FEW_SEGS = 192;
+// More workgroups than two a CU would fit for smaller heads; it pays for 32 elements only.  With 512 / 768: 2 x 4554 tokens of 23 heads of 32
+// 18.9 / 15.9, 10 x (3624 to 7249) of 4 16.8 / 15.5, fp32 8 x 8192 of 32 96.1 / 93.7; heads of 64, 2 x 4554 18.1 / 17.9, 100000 of 8 41.5 / 42.4.
+template <int HD> constexpr int PA_SLOTS = HD == 32 ? 768 : 512;
 constexpr uint32_t PA_MIN_TILES = PA_SPLIT_WAVES;   // a tile for each wave; 1 x 2048 tokens with 16 / 8 / 4: 13.8 / 12.2 / 10.9 us
 
 // Quotient of numbers that are small in all but impossible calls: a 64-bit division is 130 instructions.
@@ -370,7 +373,7 @@ struct PaCutLds { int sums[2][PA_SPLIT_WAVES], used[PA_SPLIT_WAVES], longest[PA_
 // Finds part `which` of the call (false: there are fewer).  Every thread takes a run of sequences; the one that owns the part
 // says so.  Parts of cut segments come first, whole segments, which are no longer than those, fill in behind them.
 // all_cuts: cut segments of the call.
-template <int TILE>
+template <int TILE, int SLOTS>
 __device__ __forceinline__ bool pa_find_part(const PageAttnArgs &a, int segs, int64_t which, PaCutLds &lds, PaPart &out, int &all_cuts) {
   constexpr int THREADS = PA_SPLIT_WAVES * 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -410,11 +413,11 @@ __device__ __forceinline__ bool pa_find_part(const PageAttnArgs &a, int segs, in
   uint32_t c;
   if (alike) {
     // k parts of each segment fit the card at once
-    const uint32_t k = n_segs < PA_SLOTS ? PA_SLOTS / (uint32_t)(n_segs ? n_segs : 1) : 1;
+    const uint32_t k = n_segs < SLOTS ? SLOTS / (uint32_t)(n_segs ? n_segs : 1) : 1;
     c = ((uint32_t)longest + k - 1) / k;
     c = c < PA_MIN_TILES ? PA_MIN_TILES : c;
   } else {
-    const int target = n_segs < PA_FEW_SEGS ? PA_SLOTS : PA_PARTS;
+    const int target = n_segs < PA_FEW_SEGS ? SLOTS : PA_PARTS;
     const int64_t want = pa_quotient(all_tiles + target - 1, target);
     c = want < PA_MIN_TILES ? PA_MIN_TILES : (uint32_t)want;
     // rounded up segment by segment they are more than that: longer ones, then
@@ -474,7 +477,7 @@ __global__ __launch_bounds__(PA_SPLIT_WAVES * 64, 2) void page_attn_split_kernel
   char *own = pa_lds + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * wave_bytes;
   PaPart found;
   int cuts;
-  const bool any = pa_find_part<PaGeo<T, HD>::TILE>(a, segs, blockIdx.x, cut_lds, found, cuts);
+  const bool any = pa_find_part<PaGeo<T, HD>::TILE, PA_SLOTS<HD>>(a, segs, blockIdx.x, cut_lds, found, cuts);
   if (blockIdx.x == 0 && threadIdx.x == 0) a.cuts[0] = int4{cuts, 0, 0, 0};
   if (!any) return;
   // (uniform, but read from LDS)
