@@ -270,7 +270,7 @@ def _attend_plain(s):
     batch, heads, D = Q.shape
     P, H = K.shape[1], K.shape[2]
     lens = s["seq_lens"].long()
-    top = min(s["case"]["len_max"], table.shape[1] * P)   # (rows of the table are as long as the longest sequence needs)
+    top = s["case"]["len_max"]
     t = torch.arange(top, device="cuda")
     page, at = table[:, t // P], (t % P).unsqueeze(0)
     k = K[page, at].float().permute(0, 2, 3, 1)                                   # [batch, kv head, element, token]
