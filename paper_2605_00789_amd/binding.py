@@ -382,10 +382,21 @@ def lightkv_compress_schedule_ratio(stages: StageArray, rho, tiles, grid_h, grid
 # ---- paged cache ------------------------------------------------------------------------------------------------------
 # These calls are made once a layer and token: their tensors are checked and handed on by a module of host code beside the
 # library (csrc/lk_pages_torch.cpp) -- 3 us of Python a call, otherwise, beside a launch of as many.
+class _NotLoaded:
+    """Stands for the module where it is not built, or built for another torch: the compression calls do without it, a page call
+    raises."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError("_lk_pages.so is not built or does not load (%s). Run `python paper_2605_00789_amd/build.py`." % self._why)
+
+
 try:
     from . import _lk_pages
 except ImportError as e:
-    raise ImportError("_lk_pages.so is not built or does not load (%s). Run `python paper_2605_00789_amd/build.py`." % e) from e
+    _lk_pages = _NotLoaded(e)
 
 PAGED_MAX_BATCH = 4096   # LIGHTKV_PAGED_MAX_BATCH
 # the handle of the current stream: 0.1 us, where making a torch.cuda.Stream for it takes 2.7
