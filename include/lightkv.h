@@ -526,11 +526,14 @@ typedef struct lightkv_pages {
  *   table            the new pages, behind those the sequence has; all other entries stay
  *   slots            row t in [cu_new[b], cu_new[b+1]): page * page_tokens + row in the page, of the token at position
  *                    seq_lens[b] + t - cu_new[b]; -1 if the sequence was refused (or the page number is none of the pool's).
- *                    slots has slot_rows entries; those no sequence owns stay as they were
+ *                    slots has slot_rows entries; those in front of cu_new[0] and from cu_new[batch] on stay as they were
  *   seq_lens_out     [batch] seq_lens[b] + new_b; seq_lens[b] if refused.  May be the array seq_lens itself
  *   free_count_out   [1] pages that are left.  May be free_count itself.  free_pages is only read
  *   status           [batch], may be NULL: 0; 1 where the pool ran short; 2 where the tokens do not fit the table row or
- *                    slots, or offsets or lengths are impossible (refused without a place in the order)
+ *                    slots, or offsets or lengths are impossible (refused without a place in the order).  Where offsets fall,
+ *                    the rows of a sequence are impossible, too, if they begin in front of cu_new[0] or of the end of an earlier
+ *                    sequence with possible ones, or end behind cu_new[batch]: no row has two owners, and lightkv_page_write
+ *                    with the same offsets reaches every row that got a slot; rows in between without an owner get -1
  */
 lightkv_status lightkv_page_alloc(const lightkv_pages *p, const int32_t *cu_new, const int32_t *seq_lens,
                                   const int32_t *free_pages, const int32_t *free_count, int32_t *seq_lens_out,

@@ -93,25 +93,49 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
   pg_fetch(g.cu_new, cu, g.batch + 1);
   pg_fetch(g.seq_lens, len, g.batch);
   __syncthreads();
-  int mine = 0;
-  for (int b = b0; b < b1; ++b) {
+  // pages that a sequence asks for; -2: its lengths or offsets are impossible
+  auto need_of = [&](int b) {
     const int first = cu[b], end = cu[b + 1], L = len[b];
     // (differences of any two ints: 64 bits)
     const int64_t n = (int64_t)end - first;
-    const bool over = first < 0 || n < 0 || end > g.slot_rows || L < 0 || L + n > room;
-    const int need = over ? 0 : ((int)(L + n + P - 1) >> g.lg) - ((L + P - 1) >> g.lg);
-    place[b] = over ? -2 : need;
-    mine = sat_add(mine, need);
+    if (first < 0 || n < 0 || end > g.slot_rows || L < 0 || L + n > room) return -2;
+    return ((int)(L + n + P - 1) >> g.lg) - ((L + P - 1) >> g.lg);
+  };
+  int mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int need = need_of(b);
+    place[b] = need;
+    mine = sat_add(mine, cu[b + 1] < cu[b] ? PG_SAT : (need < 0 ? 0 : need));   // offsets that fall: a sum that no pool has
   }
   int total;
   int at = wg_exclusive_sum(mine, scratch, &total), served = 0;
-  for (int b = b0; b < b1; ++b) {
-    const int need = place[b];
-    if (need < 0) continue;
-    const bool ok = need == 0 || sat_add(at, need) <= count;
-    place[b] = ok ? at : -1;
-    at = sat_add(at, need);
-    if (ok && need > 0) served = at;
+  const bool slow = total == PG_SAT;   // (the same in all threads; ascending offsets below 2^31 take 2^28 pages and one each at most)
+  if (!slow) {
+    for (int b = b0; b < b1; ++b) {
+      const int need = place[b];
+      if (need < 0) continue;
+      const bool ok = need == 0 || sat_add(at, need) <= count;
+      place[b] = ok ? at : -1;
+      at = sat_add(at, need);
+      if (ok && need > 0) served = at;
+    }
+  } else if (tid == 0) {
+    // Offsets that fall: no program should have them, so one thread decides, sequence by sequence.  A row has one owner, inside the
+    // range that a write of these offsets covers: a sequence is refused if its rows begin in front of cu[0] or of the end of
+    // one that was not, or end behind cu[batch].
+    int claimed = cu[0];
+    at = 0;
+    for (int b = 0; b < g.batch; ++b) {
+      int need = need_of(b);
+      if (need >= 0 && (cu[b] < claimed || cu[b + 1] > cu[g.batch])) need = -2;
+      place[b] = need;
+      if (need < 0) continue;
+      claimed = cu[b + 1];
+      const bool ok = need == 0 || sat_add(at, need) <= count;
+      place[b] = ok ? at : -1;
+      at = sat_add(at, need);
+      if (ok && need > 0) served = at;
+    }
   }
   if ((g.what & 2) && blockIdx.x == 0) {
     served = wave_running_max(served);
@@ -128,6 +152,21 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
   }
   if (!(g.what & 1)) return;
   const int64_t end = cu[g.batch] < g.slot_rows ? cu[g.batch] : g.slot_rows;
+  if (slow) {   // a slot at a time, its owner among all sequences
+    for (int64_t t = (int64_t)blockIdx.x * PG_THREADS + tid; t < end; t += (int64_t)gridDim.x * PG_THREADS) {
+      if (t < cu[0]) continue;
+      int b = 0, page = -1;
+      while (b < g.batch && (place[b] == -2 || t < cu[b] || t >= cu[b + 1])) ++b;
+      const int pos = b < g.batch && place[b] >= 0 ? len[b] + (int)(t - cu[b]) : -1;
+      if (pos >= 0) {
+        const int j = pos >> g.lg, old = (len[b] + P - 1) >> g.lg;
+        page = j < old ? g.table[(int64_t)b * g.table_stride + j] : g.free_pages[count - 1 - (place[b] + j - old)];
+        if (j >= old && (pos & (P - 1)) == 0) g.table[(int64_t)b * g.table_stride + j] = page;
+      }
+      g.slots[t] = (unsigned)page < (unsigned)g.n_pages ? (page << g.lg) + (pos & (P - 1)) : -1;
+    }
+    return;
+  }
   const int64_t step = (int64_t)gridDim.x * PG_THREADS * SLOTS;
   const bool wide = (reinterpret_cast<uintptr_t>(g.slots) & 15) == 0;
   for (int64_t t0 = ((int64_t)blockIdx.x * PG_THREADS + tid) * SLOTS; t0 < end; t0 += step) {
