@@ -443,10 +443,27 @@ class Pages:
         self._at, self.index = C.addressof(c), self.device.index
 
 
+def _follow(stream, current, args):
+    """A call on another stream than the current one comes behind what this one has been given so far (the arguments may have been
+    made there a line above), and memory of arguments that the caller drops is not handed out again before it has been used."""
+    states = []
+    for s in (stream, current):
+        with torch.cuda.stream(s):
+            states.append(torch.cuda.is_current_stream_capturing())
+    if states[0] != states[1]:
+        return   # one of them is being captured, which has no order with what lies outside of it
+    stream.wait_stream(current)
+    for t in args:
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            t.record_stream(stream)
+
+
 def _page_call(fn, where, p, args, stream):
     """The call on its stream: that of the cache's device, with this device current."""
     index = p.index
     s = _raw_stream(index) if stream is None else stream.cuda_stream
+    if stream is not None and s != _raw_stream(index):
+        _follow(stream, torch.cuda.current_stream(index), args)
     if _current_device() == index:
         st = fn(p._at, index, *args, s)
     else:

@@ -441,7 +441,9 @@ class PagedCache:
     each).  Everything lives on the device and no call reads it back: append (or store_stage) makes room for new tokens,
     write puts a layer's rows there, attend is one new token's attention, release takes back what finished sequences hold.
     The calls only enqueue, on the current stream or `stream`, so a decoding step can be captured into a graph and replayed.
-    Calls of one cache share its table, lengths and workspace: streams they run on must be ordered by the caller.
+    Calls of one cache share its table, lengths and workspace: streams they run on must be ordered by the caller.  (A call with
+    `stream` comes behind what the current stream has been given so far, as its arguments may; what follows on the current
+    stream does not wait for it.)
 
     pools: one (K, V) pair per layer, stored head-major inside a page ([n_pages, kv_heads, page_tokens, head_dim]: a head's
     rows of a page are one run of memory) and handed out as [n_pages, page_tokens, kv_heads, head_dim] views."""
