@@ -512,6 +512,8 @@ typedef struct lightkv_pages {
   void *K, *V;                /* device, the pools                                                              */
   int64_t k_page_stride, k_tok_stride, k_head_stride;   /* elements, not negative                               */
   int64_t v_page_stride, v_tok_stride, v_head_stride;
+  /* used by lightkv_page_alloc only                                                                            */
+  int32_t *cu_copy;           /* device [batch + 1], may be NULL: cu_new is copied there, for the writes that follow */
 } lightkv_pages;
 
 /*

@@ -55,6 +55,7 @@ class _CPages(C.Structure):
         ("K", C.c_void_p), ("V", C.c_void_p),
         ("k_page_stride", C.c_int64), ("k_tok_stride", C.c_int64), ("k_head_stride", C.c_int64),
         ("v_page_stride", C.c_int64), ("v_tok_stride", C.c_int64), ("v_head_stride", C.c_int64),
+        ("cu_copy", C.c_void_p),
     ]
 
 
@@ -409,12 +410,12 @@ class Pages:
     """Python mirror of `lightkv_pages`; keeps the tensors it points to alive.
     table: int32 [batch, max_pages].  K, V: the pools, [n_pages, page_tokens, kv_heads, head_dim] views of any strides (pages
     stored head-major are handed in as pool.transpose(1, 2)); heads: query heads.  Without K and V (tables only): n_pages
-    and page_tokens."""
+    and page_tokens.  For lightkv_page_alloc: cu_copy (int32 [batch + 1]) keeps the offsets of the last call."""
 
-    def __init__(self, table, *, K=None, V=None, heads=0, n_pages=0, page_tokens=0):
+    def __init__(self, table, *, K=None, V=None, heads=0, n_pages=0, page_tokens=0, cu_copy=None):
         if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table: int32 [batch, max_pages] with contiguous rows")
-        self.refs = (table, K, V)
+        self.refs = (table, K, V, cu_copy)
         self.device = table.device
         c = self.c = _CPages()
         c.batch, c.max_pages = int(table.shape[0]), int(table.shape[1])
@@ -439,6 +440,10 @@ class Pages:
             c.heads = int(heads) if heads else h
         else:
             c.n_pages, c.page_tokens = int(n_pages), int(page_tokens)
+        if cu_copy is not None:
+            if cu_copy.dtype != torch.int32 or cu_copy.device != self.device or not cu_copy.is_contiguous() or cu_copy.numel() <= c.batch:
+                raise ValueError("cu_copy: contiguous int32 [batch + 1] on the table's device")
+            c.cu_copy = _dptr(cu_copy)
         self._ref = C.byref(c)
         self._at, self.index = C.addressof(c), self.device.index
 

@@ -26,10 +26,10 @@ constexpr int PG_SAT = 1 << 29;            // sums of impossible lengths stop he
 
 struct AllocArgs {
   const int32_t *cu_new, *seq_lens, *free_pages, *free_count;
-  int32_t *table, *seq_lens_out, *free_count_out, *slots, *status;
+  int32_t *table, *seq_lens_out, *free_count_out, *slots, *status, *cu_copy;
   int64_t table_stride, slot_rows;
   int batch, max_pages, n_pages, lg;
-  int what;   // 1: slots and table, 2: lengths, count and status
+  int what;   // 1: slots and table, 2: lengths, count, status and the copy of the offsets
 };
 
 __device__ __forceinline__ int sat_add(int a, int b) { const int s = a + b; return s < PG_SAT ? s : PG_SAT; }
@@ -148,6 +148,8 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
       g.seq_lens_out[b] = p >= 0 ? len[b] + (cu[b + 1] - cu[b]) : len[b];
       if (g.status) g.status[b] = p >= 0 ? 0 : (p == -1 ? 1 : 2);
     }
+    if (g.cu_copy)
+      for (int i = tid; i <= g.batch; i += PG_THREADS) g.cu_copy[i] = cu[i];
     if (tid == 0) g.free_count_out[0] = count - popped;
   }
   if (!(g.what & 1)) return;
@@ -325,14 +327,15 @@ lightkv_status lightkv_page_alloc(const lightkv_pages *p, const int32_t *cu_new,
   if (!cu_new || !seq_lens || !free_pages || !free_count || !seq_lens_out || !free_count_out || !slots) return LIGHTKV_ERR_NULL;
   if (slot_rows < 0) return LIGHTKV_ERR_SHAPE;
   if (slot_rows >= (1ll << 31)) return LIGHTKV_ERR_UNSUPPORTED;
-  const void *all[] = {cu_new, seq_lens, free_pages, free_count, seq_lens_out, free_count_out, slots, status};
+  int32_t *const cu_copy = p->cu_copy == cu_new ? nullptr : p->cu_copy;   // (it has them already)
+  const void *all[] = {cu_new, seq_lens, free_pages, free_count, seq_lens_out, free_count_out, slots, status, cu_copy};
   for (const void *q : all)
     if (!aligned_to(q, 4)) return LIGHTKV_ERR_UNSUPPORTED;
   const uint64_t nb = (uint64_t)p->batch * 4, np = (uint64_t)p->n_pages * 4, nt = ((uint64_t)p->table_stride * (p->batch - 1) + p->max_pages) * 4;
   struct Range { const void *at; uint64_t bytes; };
   const Range in[] = {{cu_new, nb + 4}, {seq_lens, nb}, {free_pages, np}, {free_count, 4}};
-  const Range out[] = {{p->table, nt}, {slots, (uint64_t)slot_rows * 4}, {seq_lens_out, nb}, {free_count_out, 4}, {status, nb}};
-  for (int i = 0; i < 5; ++i) {
+  const Range out[] = {{p->table, nt}, {slots, (uint64_t)slot_rows * 4}, {seq_lens_out, nb}, {free_count_out, 4}, {status, nb}, {cu_copy, nb + 4}};
+  for (int i = 0; i < 6; ++i) {
     for (const Range &r : in) {
       if (r.at == out[i].at && ((r.at == seq_lens && i == 2) || (r.at == free_count && i == 3))) continue;
       if (overlap(r.at, r.bytes, out[i].at, out[i].bytes)) return LIGHTKV_ERR_SHAPE;
@@ -343,7 +346,7 @@ lightkv_status lightkv_page_alloc(const lightkv_pages *p, const int32_t *cu_new,
   AllocArgs g{};
   g.cu_new = cu_new; g.seq_lens = seq_lens; g.free_pages = free_pages; g.free_count = free_count; g.table = p->table;
   g.seq_lens_out = seq_lens_out; g.free_count_out = free_count_out; g.slots = slots; g.status = status;
-  g.table_stride = p->table_stride; g.slot_rows = slot_rows; g.batch = p->batch; g.max_pages = p->max_pages;
+  g.cu_copy = cu_copy; g.table_stride = p->table_stride; g.slot_rows = slot_rows; g.batch = p->batch; g.max_pages = p->max_pages;
   g.n_pages = p->n_pages; g.lg = log2_of(p->page_tokens);
   const size_t lds = (3 * (size_t)p->batch + 1) * sizeof(int);
   const bool few = slot_rows <= PG_FEW_SLOTS;

@@ -468,21 +468,22 @@ class PagedCache:
                     for _ in range(2))
             self.pools.append((K, V))
             self.pages.append(B.Pages(self.table, K=K, V=V, heads=heads))
-        self._cu_new = torch.arange(batch + 1, **i32)
-        self.one_each = self._cu_new              # cu_new of a decoding step: one token for every sequence
+        self.one_each = torch.arange(batch + 1, **i32)      # cu_new of a decoding step: one token for every sequence
+        self.cu_new = torch.zeros(batch + 1, **i32)         # that of the append that ran last, kept by the call itself
+        self._tables = B.Pages(self.table, n_pages=n_pages, page_tokens=page_tokens, cu_copy=self.cu_new)
         self.ws = torch.empty(B.lightkv_page_attention_workspace(self.pages[0]), dtype=torch.uint8, device=self.device)
 
     def append(self, cu_new: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        """Room for cu_new[b + 1] - cu_new[b] more tokens of every sequence (None: one each); the write calls that follow
-        fill it.  Returns `status` (device, see lightkv_page_alloc), which is the caller's to look at."""
-        self._cu_new = self.one_each if cu_new is None else cu_new
-        B.lightkv_page_alloc(self.pages[0], self._cu_new, self.seq_lens, self.free_pages, self.free_count, self.seq_lens,
+        """Room for cu_new[b + 1] - cu_new[b] more tokens of every sequence; the write calls that follow fill it.  None: one each.
+        Returns `status` (device, see lightkv_page_alloc), which is the caller's to look at."""
+        B.lightkv_page_alloc(self._tables, self.one_each if cu_new is None else cu_new, self.seq_lens, self.free_pages, self.free_count, self.seq_lens,
                              self.free_count, self.slots, status=self.status, stream=stream)
         return self.status
 
     def write(self, layer: int, K: torch.Tensor, V: torch.Tensor, stream=None):
-        """A layer's rows [tokens, kv_heads, head_dim] (or [tokens, kv_heads * head_dim]) of the last append."""
-        B.lightkv_page_write(self.pages[layer], self.slots, K, V, cu_new=self._cu_new, stream=stream)
+        """A layer's rows [tokens, kv_heads, head_dim] (or [tokens, kv_heads * head_dim]) of the append in front of it on the
+        device, a replayed one as well."""
+        B.lightkv_page_write(self.pages[layer], self.slots, K, V, cu_new=self.cu_new, stream=stream)
 
     def store_stage(self, layer: int, st, stream=None) -> torch.Tensor:
         """append and write of what a compression stage leaves (StageBuffers, or the EdgeStepResult of a schedule whose
@@ -500,5 +501,5 @@ class PagedCache:
 
     def release(self, done: torch.Tensor, stream=None):
         """Pages of every sequence with done[b] != 0 (int32, device) go back; its length becomes zero."""
-        B.lightkv_page_free(self.pages[0], done, self.seq_lens, self.free_pages, self.free_count, self.seq_lens,
+        B.lightkv_page_free(self._tables, done, self.seq_lens, self.free_pages, self.free_count, self.seq_lens,
                             self.free_count, stream=stream)

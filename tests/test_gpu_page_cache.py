@@ -58,3 +58,39 @@ def test_a_stream_that_is_captured_beside_the_current_one():
         ref, lens = dense([torch.stack(r) for r in rows], [torch.stack(r) for r in rows], q, 32 ** -0.5)
         check("f32", out, None, ref, 32, lens)
         torch.zeros(1000, device=DEV).sum().item()
+
+
+def test_a_write_takes_the_offsets_of_the_append_that_ran_last():
+    """A graph with an append of its own is replayed between a prompt's append and an eager write: the write is of the replayed step."""
+    import paper_2605_00789_amd as lk
+    batch, P = 3, 8
+    cache = lk.PagedCache(dtype="f32", batch=batch, heads=1, head_dim=32, n_pages=30, max_seq_tokens=64, max_new_tokens=40, page_tokens=P, layers=2)
+    k = torch.zeros(batch, 1, 32, device=DEV)
+    k.copy_(torch.arange(1.0, batch + 1, device=DEV).view(batch, 1, 1).expand_as(k))
+    cu = ints([0, 2, 4, 6])
+    cache.append(cu)
+    for layer in range(2):
+        cache.write(layer, torch.ones(6, 1, 32, device=DEV), torch.ones(6, 1, 32, device=DEV))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.append()
+        cache.write(0, k, k)
+    more = ints([5, 5, 5, 5])
+    for turn in range(3):
+        cache.append(more)                                    # nobody gets anything, and the offsets begin behind all rows of a step
+        assert cache.cu_new.tolist() == [5] * 4
+        graph.replay()
+        cache.write(1, k, 2 * k)
+        torch.zeros(1000, device=DEV).sum().item()
+        assert cache.cu_new.tolist() == [0, 1, 2, 3]
+        for b in range(batch):
+            pos = 2 + turn
+            page = int(cache.table[b, pos // P])
+            for layer, factor in ((0, 1.0), (1, 2.0)):
+                K, V = cache.pools[layer]
+                assert (K[page, pos % P] == b + 1).all() and (V[page, pos % P] == factor * (b + 1)).all()
+    cu.fill_(99)                                              # the caller's array is the caller's again
+    cache.append()
+    cache.write(0, k, k)
+    assert cache.seq_lens.tolist() == [6] * 3

@@ -192,3 +192,13 @@ def test_calls_refuse_what_is_no_tensor_of_the_cache(B):
             call()
     with pytest.raises((ValueError, TypeError)):
         ext.page_free("x", 0, i, i, i, i, i, i, 0)
+
+
+def test_the_copy_of_the_offsets(B):
+    """It is an output of lightkv_page_alloc: not in what is read, not in the other outputs; cu_new itself has them already."""
+    for where, want in ((at(20) + 2, UNSUPPORTED), (at(3) + 4, SHAPE), (at(4), SHAPE), (at(5) + 8, SHAPE), (at(6), SHAPE), (at(0) + 8, SHAPE),
+                        (at(9) + 196, SHAPE), (at(7) + 8, SHAPE), (at(8), SHAPE), (at(10), SHAPE), (at(10) - 12, SHAPE)):
+        assert _alloc(B, _pages(B, cu_copy=where)) == want, hex(where)
+        if where not in (at(7) + 8, at(8)):
+            assert _alloc(B, _pages(B, cu_copy=where), lens_out=at(4), count_out=at(6)) == want, hex(where)
+    assert _alloc(B, _pages(B, cu_copy=at(3)), lens_out=at(3)) == SHAPE
