@@ -513,6 +513,7 @@ typedef struct lightkv_pages {
   int64_t k_page_stride, k_tok_stride, k_head_stride;   /* elements, not negative                               */
   int64_t v_page_stride, v_tok_stride, v_head_stride;
   /* used by lightkv_page_alloc only                                                                            */
+  int32_t skip_empty;         /* not 0: a sequence that holds no tokens gets none (status 3): rows of a table that nobody uses */
   int32_t *cu_copy;           /* device [batch + 1], may be NULL: cu_new is copied there, for the writes that follow */
 } lightkv_pages;
 
@@ -527,15 +528,17 @@ typedef struct lightkv_pages {
  * Outputs (device):
  *   table            the new pages, behind those the sequence has; all other entries stay
  *   slots            row t in [cu_new[b], cu_new[b+1]): page * page_tokens + row in the page, of the token at position
- *                    seq_lens[b] + t - cu_new[b]; -1 if the sequence was refused (or the page number is none of the pool's).
+ *                    seq_lens[b] + t - cu_new[b]; -1 if the sequence was refused or left out (or the page number is none of
+ *                    the pool's).
  *                    slots has slot_rows entries; those in front of cu_new[0] and from cu_new[batch] on stay as they were
- *   seq_lens_out     [batch] seq_lens[b] + new_b; seq_lens[b] if refused.  May be the array seq_lens itself
+ *   seq_lens_out     [batch] seq_lens[b] + new_b; seq_lens[b] if refused or left out.  May be the array seq_lens itself
  *   free_count_out   [1] pages that are left.  May be free_count itself.  free_pages is only read
  *   status           [batch], may be NULL: 0; 1 where the pool ran short; 2 where the tokens do not fit the table row or
  *                    slots, or offsets or lengths are impossible (refused without a place in the order).  Where offsets fall,
  *                    the rows of a sequence are impossible, too, if they begin in front of cu_new[0] or of the end of an earlier
  *                    sequence with possible ones, or end behind cu_new[batch]: no row has two owners, and lightkv_page_write
- *                    with the same offsets reaches every row that got a slot; rows in between without an owner get -1
+ *                    with the same offsets reaches every row that got a slot; rows in between without an owner get -1.
+ *                    3 where skip_empty leaves the sequence out
  */
 lightkv_status lightkv_page_alloc(const lightkv_pages *p, const int32_t *cu_new, const int32_t *seq_lens,
                                   const int32_t *free_pages, const int32_t *free_count, int32_t *seq_lens_out,

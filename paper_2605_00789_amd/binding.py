@@ -55,7 +55,7 @@ class _CPages(C.Structure):
         ("K", C.c_void_p), ("V", C.c_void_p),
         ("k_page_stride", C.c_int64), ("k_tok_stride", C.c_int64), ("k_head_stride", C.c_int64),
         ("v_page_stride", C.c_int64), ("v_tok_stride", C.c_int64), ("v_head_stride", C.c_int64),
-        ("cu_copy", C.c_void_p),
+        ("skip_empty", C.c_int32), ("cu_copy", C.c_void_p),
     ]
 
 
@@ -410,9 +410,10 @@ class Pages:
     """Python mirror of `lightkv_pages`; keeps the tensors it points to alive.
     table: int32 [batch, max_pages].  K, V: the pools, [n_pages, page_tokens, kv_heads, head_dim] views of any strides (pages
     stored head-major are handed in as pool.transpose(1, 2)); heads: query heads.  Without K and V (tables only): n_pages
-    and page_tokens.  For lightkv_page_alloc: cu_copy (int32 [batch + 1]) keeps the offsets of the last call."""
+    and page_tokens.  For lightkv_page_alloc: skip_empty leaves sequences without tokens out, cu_copy (int32 [batch + 1])
+    keeps the offsets of the last call."""
 
-    def __init__(self, table, *, K=None, V=None, heads=0, n_pages=0, page_tokens=0, cu_copy=None):
+    def __init__(self, table, *, K=None, V=None, heads=0, n_pages=0, page_tokens=0, skip_empty=False, cu_copy=None):
         if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table: int32 [batch, max_pages] with contiguous rows")
         self.refs = (table, K, V, cu_copy)
@@ -440,6 +441,7 @@ class Pages:
             c.heads = int(heads) if heads else h
         else:
             c.n_pages, c.page_tokens = int(n_pages), int(page_tokens)
+        c.skip_empty = 1 if skip_empty else 0
         if cu_copy is not None:
             if cu_copy.dtype != torch.int32 or cu_copy.device != self.device or not cu_copy.is_contiguous() or cu_copy.numel() <= c.batch:
                 raise ValueError("cu_copy: contiguous int32 [batch + 1] on the table's device")

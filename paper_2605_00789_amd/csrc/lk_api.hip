@@ -246,7 +246,7 @@ const char *lightkv_status_string(int status) {
   }
 }
 
-int lightkv_version(void) { return 340; }   // 0.3.4: lightkv_pages.cu_copy (0.3.3: the paged cache; 0.3.2: lightkv_compress_schedule_ratio; 0.3.1: lightkv_problem.direction,
+int lightkv_version(void) { return 340; }   // 0.3.4: lightkv_pages.skip_empty, cu_copy (0.3.3: the paged cache; 0.3.2: lightkv_compress_schedule_ratio; 0.3.1: lightkv_problem.direction,
                                             // direction argument of lightkv_window_counts, edge lists for windows of
                                             // up to 4096 tokens)
 

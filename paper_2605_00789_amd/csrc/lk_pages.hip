@@ -28,7 +28,7 @@ struct AllocArgs {
   const int32_t *cu_new, *seq_lens, *free_pages, *free_count;
   int32_t *table, *seq_lens_out, *free_count_out, *slots, *status, *cu_copy;
   int64_t table_stride, slot_rows;
-  int batch, max_pages, n_pages, lg;
+  int batch, max_pages, n_pages, lg, skip_empty;
   int what;   // 1: slots and table, 2: lengths, count, status and the copy of the offsets
 };
 
@@ -78,7 +78,7 @@ __device__ __forceinline__ int clamped_count(const int32_t *count, int n_pages) 
   return c < 0 ? 0 : (c > n_pages ? n_pages : c);
 }
 
-// LDS: cu [batch + 1], length [batch], queue place [batch] (-1: refused)
+// LDS: cu [batch + 1], length [batch], queue place [batch], or minus the status
 template <int SLOTS>
 __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
   fetch_args<AllocArgs>();
@@ -93,19 +93,21 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
   pg_fetch(g.cu_new, cu, g.batch + 1);
   pg_fetch(g.seq_lens, len, g.batch);
   __syncthreads();
-  // pages that a sequence asks for; -2: its lengths or offsets are impossible
-  auto need_of = [&](int b) {
+  // pages that a sequence asks for; -2: its lengths or offsets are impossible, -3: it is left out
+  auto need_of = [&](int b, bool &falls) {
     const int first = cu[b], end = cu[b + 1], L = len[b];
-    // (differences of any two ints: 64 bits)
-    const int64_t n = (int64_t)end - first;
-    if (first < 0 || n < 0 || end > g.slot_rows || L < 0 || L + n > room) return -2;
-    return ((int)(L + n + P - 1) >> g.lg) - ((L + P - 1) >> g.lg);
+    const unsigned n = (unsigned)end - (unsigned)first;
+    falls = end < first;
+    const bool bad = ((first | L) < 0) | falls | (end > (int)g.slot_rows) | ((unsigned)L + n > (unsigned)room);
+    const int need = (int)(((unsigned)L + n + P - 1) >> g.lg) - (int)(((unsigned)L + P - 1) >> g.lg);
+    return bad ? -2 : (g.skip_empty && L == 0 && n != 0 ? -3 : need);
   };
   int mine = 0;
   for (int b = b0; b < b1; ++b) {
-    const int need = need_of(b);
+    bool falls;
+    const int need = need_of(b, falls);
     place[b] = need;
-    mine = sat_add(mine, cu[b + 1] < cu[b] ? PG_SAT : (need < 0 ? 0 : need));   // offsets that fall: a sum that no pool has
+    mine = sat_add(mine, falls ? PG_SAT : (need < 0 ? 0 : need));   // offsets that fall: a sum that no pool has
   }
   int total;
   int at = wg_exclusive_sum(mine, scratch, &total), served = 0;
@@ -126,11 +128,13 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
     int claimed = cu[0];
     at = 0;
     for (int b = 0; b < g.batch; ++b) {
-      int need = need_of(b);
-      if (need >= 0 && (cu[b] < claimed || cu[b + 1] > cu[g.batch])) need = -2;
+      bool falls;
+      int need = need_of(b, falls);
+      if (need != -2 && (cu[b] < claimed || cu[b + 1] > cu[g.batch])) need = -2;
       place[b] = need;
-      if (need < 0) continue;
+      if (need == -2) continue;
       claimed = cu[b + 1];
+      if (need < 0) continue;
       const bool ok = need == 0 || sat_add(at, need) <= count;
       place[b] = ok ? at : -1;
       at = sat_add(at, need);
@@ -146,7 +150,7 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
     for (int b = tid; b < g.batch; b += PG_THREADS) {
       const int p = place[b];
       g.seq_lens_out[b] = p >= 0 ? len[b] + (cu[b + 1] - cu[b]) : len[b];
-      if (g.status) g.status[b] = p >= 0 ? 0 : (p == -1 ? 1 : 2);
+      if (g.status) g.status[b] = p >= 0 ? 0 : -p;
     }
     if (g.cu_copy)
       for (int i = tid; i <= g.batch; i += PG_THREADS) g.cu_copy[i] = cu[i];
@@ -346,7 +350,7 @@ lightkv_status lightkv_page_alloc(const lightkv_pages *p, const int32_t *cu_new,
   AllocArgs g{};
   g.cu_new = cu_new; g.seq_lens = seq_lens; g.free_pages = free_pages; g.free_count = free_count; g.table = p->table;
   g.seq_lens_out = seq_lens_out; g.free_count_out = free_count_out; g.slots = slots; g.status = status;
-  g.cu_copy = cu_copy; g.table_stride = p->table_stride; g.slot_rows = slot_rows; g.batch = p->batch; g.max_pages = p->max_pages;
+  g.cu_copy = cu_copy; g.skip_empty = p->skip_empty; g.table_stride = p->table_stride; g.slot_rows = slot_rows; g.batch = p->batch; g.max_pages = p->max_pages;
   g.n_pages = p->n_pages; g.lg = log2_of(p->page_tokens);
   const size_t lds = (3 * (size_t)p->batch + 1) * sizeof(int);
   const bool few = slot_rows <= PG_FEW_SLOTS;

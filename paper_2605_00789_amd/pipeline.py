@@ -470,13 +470,17 @@ class PagedCache:
             self.pages.append(B.Pages(self.table, K=K, V=V, heads=heads))
         self.one_each = torch.arange(batch + 1, **i32)      # cu_new of a decoding step: one token for every sequence
         self.cu_new = torch.zeros(batch + 1, **i32)         # that of the append that ran last, kept by the call itself
-        self._tables = B.Pages(self.table, n_pages=n_pages, page_tokens=page_tokens, cu_copy=self.cu_new)
+        tables = dict(n_pages=n_pages, page_tokens=page_tokens, cu_copy=self.cu_new)
+        self._tables, self._step = B.Pages(self.table, **tables), B.Pages(self.table, skip_empty=True, **tables)
         self.ws = torch.empty(B.lightkv_page_attention_workspace(self.pages[0]), dtype=torch.uint8, device=self.device)
 
     def append(self, cu_new: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        """Room for cu_new[b + 1] - cu_new[b] more tokens of every sequence; the write calls that follow fill it.  None: one each.
-        Returns `status` (device, see lightkv_page_alloc), which is the caller's to look at."""
-        B.lightkv_page_alloc(self._tables, self.one_each if cu_new is None else cu_new, self.seq_lens, self.free_pages, self.free_count, self.seq_lens,
+        """Room for cu_new[b + 1] - cu_new[b] more tokens of every sequence; the write calls that follow fill it.  None: one each
+        for the sequences that hold tokens, row b of what is written being sequence b's.  Rows of the batch that hold none -- not
+        used yet, or released -- stay empty, their rows are not written (status 3); a first token of nothing is
+        append(one_each).  Returns `status` (device, see lightkv_page_alloc), which is the caller's to look at."""
+        pages, cu_new = (self._step, self.one_each) if cu_new is None else (self._tables, cu_new)
+        B.lightkv_page_alloc(pages, cu_new, self.seq_lens, self.free_pages, self.free_count, self.seq_lens,
                              self.free_count, self.slots, status=self.status, stream=stream)
         return self.status
 

@@ -44,7 +44,7 @@ def test_a_stream_that_is_captured_beside_the_current_one():
     k, q, out = torch.randn(2, 2, 32, device=DEV), torch.randn(2, 2, 32, device=DEV), torch.zeros(2, 2, 32, device=DEV)
     torch.cuda.synchronize()
     with torch.cuda.graph(graph, stream=main):
-        cache.append()
+        cache.append(cache.one_each)
         side.wait_stream(main)
         cache.write(0, k, k, stream=side)
         main.wait_stream(side)
@@ -94,3 +94,97 @@ def test_a_write_takes_the_offsets_of_the_append_that_ran_last():
     cache.append()
     cache.write(0, k, k)
     assert cache.seq_lens.tolist() == [6] * 3
+
+
+def test_a_row_that_was_released_stays_empty_until_it_is_filled():
+    """A captured step, replayed for more than a page's tokens while one row of the batch is released and one was never used: these take
+    no page from the others, and row b of what is written stays sequence b's."""
+    import paper_2605_00789_amd as lk
+    batch, P, H, D = 4, 8, 2, 32
+    # pages for three sequences of 21 tokens and not one more
+    cache = lk.PagedCache(dtype="f32", batch=batch, heads=H, head_dim=D, n_pages=9, max_seq_tokens=64, max_new_tokens=40, page_tokens=P)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, q, out = (torch.zeros(batch, H, D, device=DEV) for _ in range(3))
+    lse = torch.zeros(H, batch, device=DEV)
+    rows = [torch.zeros(0, H, D, device=DEV) for _ in range(batch)]
+
+    def fill(b, n):
+        x = torch.randn(n, H, D, generator=g, device=DEV)
+        status = cache.append(ints([0] * (b + 1) + [n] * (batch - b)))
+        cache.write(0, x, 2 * x)
+        rows[b] = x
+        assert status.tolist() == [0] * batch
+
+    def compare(status):
+        ref, lens = dense(rows, [2 * r for r in rows], q, D ** -0.5)
+        check("f32", out, lse, ref, D, lens)
+        assert cache.seq_lens.tolist() == lens and cache.status.tolist() == status
+        assert int(cache.free_count) == 9 - sum(-(-n // P) for n in lens)
+        assert (out[[b for b in range(batch) if lens[b] == 0]] == 0).all()
+
+    for b in (0, 1, 3):
+        fill(b, 3)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.append()
+        cache.write(0, k, 2 * k)
+        cache.attend(0, q, out, lse=lse)
+    def replay():
+        for x in (k, q):
+            x.copy_(torch.randn(batch, H, D, generator=g, device=DEV))
+        graph.replay()
+        for b in range(batch):
+            if len(rows[b]):
+                rows[b] = torch.cat([rows[b], k[b:b + 1]])
+        torch.zeros(1000, device=DEV).sum().item()
+
+    for _ in range(6):
+        replay()
+        compare([0, 0, 3, 0])
+    cache.release(ints([0, 1, 0, 0]))
+    rows[1] = rows[1][:0]
+    for _ in range(12):
+        replay()
+        compare([0, 3, 3, 0])
+    assert cache.seq_lens.tolist() == [21, 0, 0, 21]
+    fill(2, 9)                                                # another request takes the row that was never used
+    fill(1, 1)
+    for _ in range(3):
+        replay()
+        compare([0] * batch)
+
+
+def test_a_first_token_of_nothing():
+    """append() gives nothing to empty sequences, append(one_each) does."""
+    import paper_2605_00789_amd as lk
+    cache = lk.PagedCache(dtype="bf16", batch=2, heads=1, head_dim=32, n_pages=4, max_seq_tokens=16, max_new_tokens=4)
+    assert cache.append().tolist() == [3, 3] and cache.seq_lens.tolist() == [0, 0] and cache.slots[:2].tolist() == [-1, -1]
+    assert cache.append(cache.one_each).tolist() == [0, 0] and cache.seq_lens.tolist() == [1, 1]
+    assert cache.append().tolist() == [0, 0] and cache.seq_lens.tolist() == [2, 2] and int(cache.free_count) == 2
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("rows", [70, 3000])
+def test_sequences_without_tokens_are_left_out(rows, in_place):
+    """skip_empty among prompts, empty prompts, impossible lengths, offsets that fall and a pool that runs short."""
+    from paper_2605_00789_amd import binding as B
+    P, lens = 8, [0, 3, 0, -2, 8, 0, 5]
+    for cu, status, grown in (([0, 2, 4, 4, 6, 8, 10, 40], [3, 0, 0, 2, 0, 3, 1], [0, 5, 0, -2, 10, 0, 5]),
+                              ([0, 4, 6, 6, 5, 7, 9, 12], [3, 0, 0, 2, 2, 3, 0], [0, 5, 0, -2, 8, 0, 8])):
+        table = torch.full((7, 6), -5, **I32)
+        table[1, 0], table[4, 0], table[6, 0] = 9, 8, 7
+        pages = B.Pages(table, n_pages=10, page_tokens=P, skip_empty=True)
+        old, count = ints(lens), ints([2])
+        new, left = (old, count) if in_place else (torch.full_like(old, 99), torch.full_like(count, 99))
+        slots, st = torch.full((rows,), -7, **I32), torch.full_like(old, 99)
+        B.lightkv_page_alloc(pages, ints(cu), old, ints([5, 6, 0, 0, 0, 0, 0, 0, 0, 0]), count, new, left, slots, status=st)
+        assert st.tolist() == status and new.tolist() == grown and left.tolist() == [1 if status[4] == 0 else 2]
+        want = [-7] * rows
+        for t in range(cu[-1]):
+            want[t] = -1
+            for b in range(7):
+                if status[b] == 0 and cu[b] <= t < cu[b + 1]:
+                    pos = lens[b] + t - cu[b]
+                    want[t] = (6 if b == 4 else int(table[b, 0])) * P + pos % P
+        assert slots.tolist() == want
