@@ -583,10 +583,11 @@ lightkv_status lightkv_page_attention_workspace(const lightkv_pages *p, size_t *
  *   max_seq_tokens  the caller's bound on seq_lens if it has one (0: max_pages * page_tokens).  It chooses how the work is
  *              cut, nothing else: longer sequences are attended to in full
  *   ws         two calls that share it must be ordered by their streams
- * Scores, softmax and sums are fp32; weights enter the product with bf16 values as the sum of two bf16 numbers.  Where the
- * length is split, the cut depends on the lengths of all sequences of the call, so the last bits of a sequence may differ in
- * another batch; the same call gives the same bits.  Weights below the smallest fp32 number are zero, also against an
- * infinity.  One launch, or two where the bound lets a sequence be long (more than 768 tokens; 2048 with 160 or more pairs
+ * Scores, softmax and sums are fp32; weights enter the product with bf16 values as the sum of two bf16 numbers, off by 2^-15 of
+ * themselves or by 2^-133.  Where the length is split, the cut depends on the lengths of all sequences of the call, so the last
+ * bits of a sequence may differ in another batch; the same call gives the same bits.  A weight below 2^-126 may count as zero, also
+ * against an infinity (0 * inf: NaN); any other gives an infinity.  A score of +inf leaves NaN in out and lse (inf - inf).
+ * One launch, or two where the bound lets a sequence be long (more than 768 tokens; 2048 with 160 or more pairs
  * of a sequence and a K/V head).
  */
 lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq_lens, int32_t max_seq_tokens,

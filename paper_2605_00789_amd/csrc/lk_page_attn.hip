@@ -174,9 +174,10 @@ __device__ __forceinline__ void pa_accumulate(PaState<T, HD> &st, PaTile<T, HD> 
     for (int j = 0; j < 4; ++j) {
       const uint32_t a = __float_as_uint(p[j >> 1][(j & 1) * 2]), b = __float_as_uint(p[j >> 1][(j & 1) * 2 + 1]);
       hi[j] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-      // (a little more than the rest: a weight that one bf16 number holds must not meet an infinity with a zero)
-      const float ra = fmaf(p[j >> 1][(j & 1) * 2], 0x1p-24f, __uint_as_float(a) - __uint_as_float(a & 0xffff0000u));
-      const float rb = fmaf(p[j >> 1][(j & 1) * 2 + 1], 0x1p-24f, __uint_as_float(b) - __uint_as_float(b & 0xffff0000u));
+      // (never zero where the weight is not: a weight that one bf16 number holds must not meet an infinity with a zero.  At least
+      // the smallest bf16 number, 2^-133, then, which the matrix instruction keeps; at most the weight)
+      const float ra = __builtin_amdgcn_fmed3f(__uint_as_float(a) - __uint_as_float(a & 0xffff0000u), 0x1p-133f, __uint_as_float(a));
+      const float rb = __builtin_amdgcn_fmed3f(__uint_as_float(b) - __uint_as_float(b & 0xffff0000u), 0x1p-133f, __uint_as_float(b));
       lo[j] = __builtin_amdgcn_perm(__float_as_uint(rb), __float_as_uint(ra), 0x07060302u);
     }
     const bf16x8 ph = __builtin_bit_cast(bf16x8, uint4{hi[0], hi[1], hi[2], hi[3]}), pl = __builtin_bit_cast(bf16x8, uint4{lo[0], lo[1], lo[2], lo[3]});

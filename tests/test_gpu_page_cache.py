@@ -188,3 +188,32 @@ def test_sequences_without_tokens_are_left_out(rows, in_place):
                     pos = lens[b] + t - cu[b]
                     want[t] = (6 if b == 4 else int(table[b, 0])) * P + pos % P
         assert slots.tolist() == want
+
+
+@pytest.mark.parametrize("hint", [1, 1 << 20], ids=["whole", "split"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinities_under_the_smallest_weights(dtype, hint):
+    """Weights of 2^-1 to 2^-126, numbers that one bf16 value holds, against rows with infinities; and against the largest finite value, where
+    a weight may be off by 2^-15 of itself or by 2^-133, as its two bf16 parts allow (fp32: 2^-22, the exponential's)."""
+    from paper_2605_00789_amd import binding as B
+    n, D, P, dt = 126, 32, 8, {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    K, V = (torch.zeros(n, P, 1, D, dtype=dt, device=DEV) for _ in range(2))
+    K[:, 1, 0, 0] = -torch.arange(1.0, n + 1, device=DEV).to(dt)
+    V[:, :2, 0, 1] = 3.0
+    V[:, 1, 0, 0], V[:, 1, 0, 2] = float("inf"), float("-inf")
+    V[:, 0, 0, 3], V[:, 1, 0, 3] = 1.0, 2.0 ** 127
+    Q, out = torch.zeros(n, 1, D, dtype=dt, device=DEV), torch.empty(n, 1, D, dtype=dt, device=DEV)
+    Q[:, 0, 0] = 1.0
+    ws = torch.empty(B.lightkv_page_attention_workspace(B.Pages(torch.zeros(n, 1, **I32), K=K, V=V)), dtype=torch.uint8, device=DEV)
+    # 0.6931472 * log2(e) is 1 in fp32: the exponents are whole numbers
+    B.lightkv_page_attention(B.Pages(torch.arange(n, **I32).view(n, 1), K=K, V=V), ints([2] * n), Q, out, ws, softmax_scale=0.6931471824645996, max_seq_tokens=hint)
+    got = out[:, 0].double().cpu()
+    assert (got[:, 0] == float("inf")).all() and (got[:, 2] == -float("inf")).all()
+    step = torch.finfo(dt).eps / 2
+    w = 2.0 ** -torch.arange(1, n + 1, dtype=torch.float64)
+    off = w * 2.0 ** -22 + (torch.maximum(w * 2.0 ** -15, torch.tensor(2.0 ** -133, dtype=torch.float64)) if dtype == "bf16" else 0)
+    for e, big in ((1, 3.0), (3, 2.0 ** 127)):
+        want = (big * w + (3.0 if e == 1 else 1.0)) / (1 + w)
+        # the weights' errors against their values, twice (sum and quotient), four roundings in fp32, one to the result's type
+        tol = 2 * off * big + want * 4 * 2.0 ** -24
+        assert ((got[:, e] - want).abs() <= tol + step * (want + tol)).all(), e
