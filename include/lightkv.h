@@ -578,7 +578,7 @@ lightkv_status lightkv_page_attention_workspace(const lightkv_pages *p, size_t *
  * -inf, gets out = 0 and lse = -inf.  Tokens whose table entry is no page of the pool are left out.  NaN and infinities in
  * rows behind the last token do not reach the result; those of rows that count do, as the formula says.
  *   Q, out     element (b, h, e) at Q[b*q_tok_stride + h*q_head_stride + e], out alike; they must not overlap
- *   softmax_scale   0 selects 1/sqrt(head_dim)
+ *   softmax_scale   0 selects 1/sqrt(head_dim); 2.3e38 at most (times log2(e) it has to stay a number)
  *   lse        [heads, batch] natural logarithm, may be NULL
  *   max_seq_tokens  the caller's bound on seq_lens if it has one (0: max_pages * page_tokens).  It chooses how the work is
  *              cut, nothing else: longer sequences are attended to in full

@@ -660,7 +660,8 @@ lightkv_status lightkv_page_attention(const lightkv_pages *p, const int32_t *seq
   lightkv_status st = check_page_attention(p);
   if (st != LIGHTKV_OK) return st;
   if (!seq_lens || !Q || !out) return LIGHTKV_ERR_NULL;
-  if (!(softmax_scale >= 0.f && softmax_scale <= 3.4e38f) || max_seq_tokens < 0) return LIGHTKV_ERR_SHAPE;   // (NaN too)
+  // (NaN too; scores are taken times scale * log2(e), which has to be a number)
+  if (!(softmax_scale >= 0.f && softmax_scale * PA_LOG2E <= 3.4028234e38f) || max_seq_tokens < 0) return LIGHTKV_ERR_SHAPE;
   if (!aligned_to(seq_lens, 4) || !aligned_to(lse, 4)) return LIGHTKV_ERR_UNSUPPORTED;
   const int eb = page_elem_bytes(p);
   st = check_strided(Q, eb, q_tok_stride, p->batch, q_head_stride, p->heads);

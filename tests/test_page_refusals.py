@@ -202,3 +202,9 @@ def test_the_copy_of_the_offsets(B):
         if where not in (at(7) + 8, at(8)):
             assert _alloc(B, _pages(B, cu_copy=where), lens_out=at(4), count_out=at(6)) == want, hex(where)
     assert _alloc(B, _pages(B, cu_copy=at(3)), lens_out=at(3)) == SHAPE
+
+
+def test_the_largest_scale(B):
+    """Scores are taken times scale * log2(e): a scale that overflows there is refused, the largest one below is not (WORKSPACE: past it)."""
+    for scale, want in ((2.4e38, SHAPE), (3.4e38, SHAPE), (2.35e38, WORKSPACE), (1e-45, WORKSPACE), (3.5e38, SHAPE)):
+        assert _attend(B, _pages(B), scale=scale, ws=None) == want, scale
