@@ -126,6 +126,12 @@ PyObject *page_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   return guarded(n_args, 10, [&] {
     const Cache c = cache_of(a[0], a[1]);
     const int64_t n = c.p->batch, heads = c.p->heads;
+    const double scale = PyFloat_AsDouble(a[7]);
+    const long bound = PyLong_AsLong(a[8]);
+    if (PyErr_Occurred()) throw Refused("softmax_scale, max_seq_tokens: numbers expected");
+    if (bound < INT32_MIN || bound > INT32_MAX) throw Refused("max_seq_tokens: beyond 32 bits");
+    // (zero stands for 1 / sqrt(head_dim))
+    if (scale != 0 && (float)scale == 0) throw Refused("softmax_scale: too small for 32 bits");
     const int32_t *lens = ints(a[2], n, c, "seq_lens");
     const Rows q = rows(a[3], heads, n, c, "Q"), out = rows(a[4], heads, n, c, "out");
     const at::Tensor &ws = tensor_of(a[5], "ws");
@@ -136,10 +142,6 @@ PyObject *page_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
       if (t.scalar_type() != at::kFloat || !on_device(t, c) || t.numel() < heads * n || !t.is_contiguous()) throw Refused("lse: contiguous float32 [heads, batch] on the table's device");
       lse = static_cast<float *>(t.data_ptr());
     }
-    const double scale = PyFloat_AsDouble(a[7]);
-    const long bound = PyLong_AsLong(a[8]);
-    if (PyErr_Occurred()) throw Refused("softmax_scale, max_seq_tokens: numbers expected");
-    if (bound < INT32_MIN || bound > INT32_MAX) throw Refused("max_seq_tokens: beyond 32 bits");
     void *s = stream_of(a[9]), *ws_at = ws.data_ptr();
     const size_t ws_bytes = ws.nbytes();
     return without_lock([&] {

@@ -208,3 +208,12 @@ def test_the_largest_scale(B):
     """Scores are taken times scale * log2(e): a scale that overflows there is refused, the largest one below is not (WORKSPACE: past it)."""
     for scale, want in ((2.4e38, SHAPE), (3.4e38, SHAPE), (2.35e38, WORKSPACE), (1e-45, WORKSPACE), (3.5e38, SHAPE)):
         assert _attend(B, _pages(B), scale=scale, ws=None) == want, scale
+
+
+def test_a_scale_that_rounds_to_zero(B):
+    """Zero selects the default: a scale that only becomes zero in fp32 must not."""
+    import torch
+    p, host = _pages(B), torch.zeros(3, 8, 64, dtype=torch.bfloat16)
+    for scale, what in ((1e-46, "softmax_scale"), (-1e-300, "softmax_scale"), (1e-44, "seq_lens"), (0.0, "seq_lens")):
+        with pytest.raises(ValueError, match=what):
+            B._lk_pages.page_attention(C.addressof(p), 0, 3.5, host, host, host, None, scale, 0, 0)
