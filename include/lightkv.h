@@ -562,7 +562,8 @@ lightkv_status lightkv_page_free(const lightkv_pages *p, const int32_t *done, co
  * slots[t] % page_tokens of page slots[t] / page_tokens of the pools.  Rows cu_new[0] <= t < min(rows, cu_new[batch]) are looked
  * at (all `rows` if cu_new is NULL); a slot that is negative or behind the pool's last page leaves its row out.  K or V may be NULL
  * (skipped).  Slots should differ: of two rows with one slot, either may be found there afterwards, in parts too.
- * The rows must not overlap the pools.
+ * The rows, slots and cu_new must not overlap the pools; pools that are written together may lie in each other's gaps (pages of one
+ * allocation in turn, say) but not share elements.
  */
 lightkv_status lightkv_page_write(const lightkv_pages *p, const int32_t *cu_new, const int32_t *slots, int64_t rows,
                                   const void *K, int64_t k_tok_stride, int64_t k_head_stride,

@@ -89,6 +89,40 @@ inline uint64_t pool_bytes(const lightkv_pages *p, int64_t page_stride, int64_t 
          + (uint64_t)tok_stride * (uint64_t)(p->page_tokens - 1) * (uint64_t)page_elem_bytes(p);
 }
 
+// Whether elements of V's rows, `delta` elements behind K's, are elements of K's rows.  Axes in the order of falling strides, each of them
+// wider than what lies inside it (apart()); `stride` holds K's and V's.  Exact where both have the same strides; axes that differ
+// count as filled.
+inline bool rows_meet(int64_t delta, int64_t run, const int64_t (*stride)[2], const int64_t *count, int axes) {
+  int64_t extent[2] = {run, run};
+  for (int i = 0; i < axes; ++i)
+    for (int k = 0; k < 2; ++k) extent[k] += stride[i][k] * (count[i] - 1);
+  if (delta >= extent[0] || -delta >= extent[1]) return false;
+  if (axes == 0 || stride[0][0] != stride[0][1]) return true;
+  // entry i of K's axis against entry i + d of V's
+  const int64_t s = stride[0][0], near = -delta / s;
+  for (int64_t d = near - 2; d <= near + 2; ++d)
+    if (d > -count[0] && d < count[0] && rows_meet(delta + d * s, run, stride + 1, count + 1, axes - 1)) return true;
+  return false;
+}
+
+// Whether the pools of keys and values share elements (each of them apart in itself).
+inline bool pools_meet(const lightkv_pages *p) {
+  const int64_t all[3][2] = {{p->k_page_stride, p->v_page_stride}, {p->k_tok_stride, p->v_tok_stride}, {p->k_head_stride, p->v_head_stride}};
+  const int64_t n[3] = {p->n_pages, p->page_tokens, p->kv_heads};
+  int64_t stride[3][2], count[3];
+  int axes = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] < 2) continue;
+    int at = axes++;
+    for (; at > 0 && stride[at - 1][0] < all[i][0]; --at) {
+      stride[at][0] = stride[at - 1][0]; stride[at][1] = stride[at - 1][1]; count[at] = count[at - 1];
+    }
+    stride[at][0] = all[i][0]; stride[at][1] = all[i][1]; count[at] = n[i];
+  }
+  const intptr_t bytes = reinterpret_cast<intptr_t>(p->V) - reinterpret_cast<intptr_t>(p->K);
+  return rows_meet(bytes / page_elem_bytes(p), p->head_dim, stride, count, axes);
+}
+
 // ---- device ----
 // Loads and stores of memory that is touched once: they do not stay in the caches.
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;

@@ -430,7 +430,11 @@ lightkv_status lightkv_page_write(const lightkv_pages *p, const int32_t *cu_new,
     const uint64_t n = strided_bytes(eb, tok[i], rows, head[i], p->kv_heads, p->head_dim);
     for (int k = 0; k < 2; ++k)
       if (src[k] && overlap(src[i], n, dst[k], pool_bytes(p, page_s[k], tok_s[k], head_s[k]))) return LIGHTKV_ERR_SHAPE;
+    // slots and offsets are read while pools are written
+    const uint64_t bytes = pool_bytes(p, page_s[i], tok_s[i], head_s[i]);
+    if (overlap(slots, (uint64_t)rows * 4, dst[i], bytes) || overlap(cu_new, ((uint64_t)p->batch + 1) * 4, dst[i], bytes)) return LIGHTKV_ERR_SHAPE;
   }
+  if (K && V && pools_meet(p)) return LIGHTKV_ERR_SHAPE;   // keys and values would be written over each other
   if (rows == 0) return LIGHTKV_OK;
   WriteArgs g{};
   g.cu_new = cu_new; g.slots = slots; g.rows = rows; g.batch = p->batch; g.n_slots = p->n_pages * p->page_tokens; g.lg = log2_of(p->page_tokens);

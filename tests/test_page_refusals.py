@@ -217,3 +217,61 @@ def test_a_scale_that_rounds_to_zero(B):
     for scale, what in ((1e-46, "softmax_scale"), (-1e-300, "softmax_scale"), (1e-44, "seq_lens"), (0.0, "seq_lens")):
         with pytest.raises(ValueError, match=what):
             B._lk_pages.page_attention(C.addressof(p), 0, 3.5, host, host, host, None, scale, 0, 0)
+
+
+def test_a_write_and_what_it_reads(B):
+    """Slots and offsets are read while the pools are written."""
+    end = at(1) + 10 * 16 * 128 * 2
+    for o in (dict(slots=at(1)), dict(slots=at(2) + 4096), dict(slots=end - 4), dict(slots=at(1) - 196), dict(cu=at(2)), dict(cu=end - 4), dict(cu=at(1) - 12)):
+        assert _write(B, _pages(B), **o) == SHAPE, o
+
+
+def test_pools_that_lie_in_each_other(B):
+    """Keys and values of one allocation: in turn they are fine, shared elements are not (no rows: nothing is launched)."""
+    def both(off, page, tok, head, **over):
+        return _pages(B, K=at(1), V=at(1) + 2 * off, k_page_stride=page, v_page_stride=page, k_tok_stride=tok, v_tok_stride=tok,
+                      k_head_stride=head, v_head_stride=head, **over)
+    for off, page, tok, head in ((2048, 4096, 128, 64), (-2048, 4096, 128, 64), (128, 4096, 256, 64), (64, 4096, 256, 128), (20480, 2048, 128, 64), (-20480, 2048, 128, 64),
+                                 (1280, 128, 2560, 64), (64, 4096, 128, 2048), (64, 256, 2560, 128), (2048 + 3 * 4096, 4096, 128, 64)):
+        assert _write(B, both(off, page, tok, head), rows=0) == OK, (off, page, tok, head)
+    for off, page, tok, head in ((0, 2048, 128, 64), (2048, 2048, 128, 64), (-2048, 2048, 128, 64), (64, 4096, 128, 64), (128, 4096, 128, 64), (2048 - 64, 4096, 128, 64),
+                                 (2048 + 64, 4096, 128, 64), (9 * 4096, 4096, 128, 64), (9 * 4096 + 2048 - 32, 4096, 128, 64), (32, 4096, 256, 128), (96, 4096, 256, 128),
+                                 (20480 - 64, 2048, 128, 64), (-20480 + 8, 2048, 128, 64), (4096 * 2 + 256 * 3 + 64, 4096, 256, 64)):
+        assert _write(B, both(off, page, tok, head), rows=0) == SHAPE, (off, page, tok, head)
+        assert _write(B, both(off, page, tok, head), rows=0, V=None) == OK      # one of them alone
+    # strides inside a page that differ: pages in turn are told apart, anything closer is refused
+    over = dict(K=at(1), k_page_stride=4096, v_page_stride=4096)
+    assert _write(B, _pages(B, V=at(1) + 4096, **over), rows=0) == OK and _write(B, _pages(B, V=at(1) + 4096 - 128, **over), rows=0) == SHAPE
+    assert _write(B, _pages(B, V=at(1)), rows=0) == SHAPE
+    # one page, one head: axes of one entry do not count
+    assert _write(B, both(2048, 0, 128, 64, n_pages=1), rows=0) == OK and _write(B, both(64, 0, 128, 7, n_pages=1, kv_heads=1), rows=0) == OK
+    assert _write(B, both(32, 0, 128, 64, n_pages=1, kv_heads=1), rows=0) == SHAPE
+    # attention only reads them: the same rows may be keys and values
+    assert _attend(B, both(0, 2048, 128, 64), ws=None) == WORKSPACE
+
+
+def test_pools_that_lie_in_each_other_against_every_element(B):
+    """The same question answered by listing the elements, for strides and distances drawn at random."""
+    import itertools
+    import random
+    rng = random.Random(5)
+    told = {True: 0, False: 0}
+    for _ in range(400):
+        n, P, H, D = rng.choice([1, 2, 3]), 8, rng.choice([1, 2, 3]), 32
+        axes = [("page", n), ("tok", P), ("head", H)]
+        rng.shuffle(axes)
+        width, stride = D, {}
+        for name, k in axes:
+            stride[name] = width + rng.choice([0, 0, 32, 64])
+            width = stride[name] * (k - 1) + width
+            width += -width % 8
+        def elements(at0):
+            return {at0 + i * stride["page"] + t * stride["tok"] + h * stride["head"] + e for i, t, h in itertools.product(range(n), range(P), range(H)) for e in range(0, D, 8)}
+        off = rng.randrange(-width - 64, width + 64) // 8 * 8 if rng.random() < 0.5 else rng.choice([-1, 1]) * (rng.randrange(n + 1) * stride["page"] + rng.randrange(2) * stride["tok"]
+                                                                                                          + rng.randrange(2) * stride["head"] + rng.choice([0, 0, 32, 64]))
+        shared = bool(elements(0) & elements(off))
+        told[shared] += 1
+        p = _pages(B, n_pages=n, page_tokens=P, kv_heads=H, heads=H, head_dim=D, K=at(3), V=at(3) + 2 * off,
+                   **{"%s_%s_stride" % (kv, name): s for name, s in stride.items() for kv in "kv"})
+        assert _write(B, p, rows=0, kh=32, vh=32, kt=32 * H, vt=32 * H, slots=at(30), cu=None, K=at(31), V=at(32)) == (SHAPE if shared else OK), (n, H, stride, off)
+    assert min(told.values()) > 80, told
