@@ -406,6 +406,14 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 _PAGE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
+def _int32(value, what):
+    """A size for the descriptor: its fields would keep the low 32 bits of a larger number."""
+    value = int(value)
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError("%s: %d is beyond 32 bits" % (what, value))
+    return value
+
+
 class Pages:
     """Python mirror of `lightkv_pages`; keeps the tensors it points to alive.
     table: int32 [batch, max_pages].  K, V: the pools, [n_pages, page_tokens, kv_heads, head_dim] views of any strides (pages
@@ -414,6 +422,10 @@ class Pages:
     keeps the offsets of the last call."""
 
     def __init__(self, table, *, K=None, V=None, heads=0, n_pages=0, page_tokens=0, skip_empty=False, cu_copy=None):
+        heads, n_pages, page_tokens = (_int32(v, what) for v, what in ((heads, "heads"), (n_pages, "n_pages"), (page_tokens, "page_tokens")))
+        for what, t in (("table", table), ("K", K), ("V", V)):
+            for size in () if t is None else t.shape:
+                _int32(size, what)
         if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table: int32 [batch, max_pages] with contiguous rows")
         self.refs = (table, K, V, cu_copy)
@@ -438,9 +450,9 @@ class Pages:
             if n_pages not in (0, n) or page_tokens not in (0, p):
                 raise ValueError("n_pages or page_tokens differ from the pools'")
             c.n_pages, c.page_tokens, c.kv_heads, c.head_dim, c.dtype = n, p, h, d, _PAGE_DTYPES[self.dtype]
-            c.heads = int(heads) if heads else h
+            c.heads = heads if heads else h
         else:
-            c.n_pages, c.page_tokens = int(n_pages), int(page_tokens)
+            c.n_pages, c.page_tokens = n_pages, page_tokens
         c.skip_empty = 1 if skip_empty else 0
         if cu_copy is not None:
             if cu_copy.dtype != torch.int32 or cu_copy.device != self.device or not cu_copy.is_contiguous() or cu_copy.numel() <= c.batch:
