@@ -493,6 +493,7 @@ class PagedCache:
         """append and write of what a compression stage leaves (StageBuffers, or the EdgeStepResult of a schedule whose
         counts depend on the data): the lengths are taken from its cu_vis_out on the device."""
         K, V = (st.K_out, st.V_out) if isinstance(st, StageBuffers) else (st.K, st.V)
+        B.lightkv_page_write(self.pages[layer], self.slots[:0], K, V)   # (no row: refuses another type, width or layer before tokens are counted)
         status = self.append(st.cu_vis_out, stream=stream)
         self.write(layer, K, V, stream=stream)
         return status

@@ -217,3 +217,17 @@ def test_infinities_under_the_smallest_weights(dtype, hint):
         # the weights' errors against their values, twice (sum and quotient), four roundings in fp32, one to the result's type
         tol = 2 * off * big + want * 4 * 2.0 ** -24
         assert ((got[:, e] - want).abs() <= tol + step * (want + tol)).all(), e
+
+
+def test_a_stage_that_does_not_fit_leaves_the_cache_as_it_was():
+    """Rows of another type, width or layer: refused before any sequence is given tokens that are never written."""
+    import types
+    import paper_2605_00789_amd as lk
+    cache = lk.PagedCache(dtype="bf16", batch=2, heads=4, head_dim=32, n_pages=9, max_seq_tokens=64, max_new_tokens=40)
+    def stage(dtype=torch.bfloat16, width=128):
+        return types.SimpleNamespace(K=torch.zeros(10, width, dtype=dtype, device=DEV), V=torch.zeros(10, width, dtype=dtype, device=DEV), cu_vis_out=ints([0, 4, 10]))
+    for layer, st, error in ((0, stage(torch.float32), ValueError), (0, stage(width=96), ValueError), (1, stage(), IndexError)):
+        with pytest.raises(error):
+            cache.store_stage(layer, st)
+        assert cache.seq_lens.tolist() == [0, 0] and int(cache.free_count) == 9
+    assert cache.store_stage(0, stage()).tolist() == [0, 0] and cache.seq_lens.tolist() == [4, 6]
