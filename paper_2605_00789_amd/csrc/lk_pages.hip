@@ -73,6 +73,25 @@ __device__ __forceinline__ void pg_fetch(const int32_t *from, int *to, int n) {
   }
 }
 
+// n + 1 offsets and n lengths, all of a thread's loads on their way at once.
+__device__ __forceinline__ void pg_fetch_both(const int32_t *cu, int *to_cu, const int32_t *len, int *to_len, int n) {
+  for (int i0 = threadIdx.x; i0 <= n; i0 += 2 * PG_THREADS) {
+    int c[2], l[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int i = i0 + u * PG_THREADS;
+      c[u] = i <= n ? cu[i] : 0;
+      l[u] = i < n ? len[i] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int i = i0 + u * PG_THREADS;
+      if (i <= n) to_cu[i] = c[u];
+      if (i < n) to_len[i] = l[u];
+    }
+  }
+}
+
 __device__ __forceinline__ int clamped_count(const int32_t *count, int n_pages) {
   const int c = count[0];
   return c < 0 ? 0 : (c > n_pages ? n_pages : c);
@@ -90,8 +109,7 @@ __global__ __launch_bounds__(PG_THREADS) void page_alloc_kernel(AllocArgs g) {
   const int room = g.max_pages << g.lg, P = 1 << g.lg;
   const int per = (g.batch + PG_THREADS - 1) / PG_THREADS, b0 = tid * per, b1 = b0 + per < g.batch ? b0 + per : g.batch;
   if (tid == 0) popped = 0;
-  pg_fetch(g.cu_new, cu, g.batch + 1);
-  pg_fetch(g.seq_lens, len, g.batch);
+  pg_fetch_both(g.cu_new, cu, g.seq_lens, len, g.batch);
   __syncthreads();
   // pages that a sequence asks for; -2: its lengths or offsets are impossible, -3: it is left out
   auto need_of = [&](int b, bool &falls) {
