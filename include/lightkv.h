@@ -514,7 +514,8 @@ typedef struct lightkv_pages {
   int64_t v_page_stride, v_tok_stride, v_head_stride;
   /* used by lightkv_page_alloc only                                                                            */
   int32_t skip_empty;         /* not 0: a sequence that holds no tokens gets none (status 3): rows of a table that nobody uses */
-  int32_t *cu_copy;           /* device [batch + 1], may be NULL: cu_new is copied there, for the writes that follow */
+  int32_t *cu_copy;           /* device [batch + 1], may be NULL: cu_new is copied there, for the writes that follow.  It must not overlap
+                                 the call's other arrays; where it is cu_new itself nothing is copied */
 } lightkv_pages;
 
 /*

@@ -354,7 +354,8 @@ constexpr int PA_SPLIT_WAVES = 4, PA_JOIN_THREADS = 256;
 // fit the card, two workgroups of 256 registers a CU.  Otherwise twice as many, so that what is left at the end is small.
 // us a call with 512 / 1024, 8 K/V heads unless named: 131000 tokens 94.3 / 97.6, 16 x 1100 tokens of 32 heads 52.1 / 56.7, 16 x 8192 of 4
 // heads 55.4 / 61.9, 3 x (1 to 8000) of 32 heads 39.6 / 43.0; 64 x (1 to 8192) 193.9 / 176.2, 16 x (50 to 2000) of 32 heads
-// 66.4 / 54.1, 64 x (1 to 4096) 104.4 / 93.5, 24 x (1 to 16000) 134.8 / 128.6.
+// 66.4 / 54.1, 64 x (1 to 4096) 104.4 / 93.5, 24 x (1 to 16000) 134.8 / 128.6.  Alike segments that are more than half of what fits
+// are not cut, and a last round that is not full costs: 4096 tokens of 512 segments 171 us, 6.3 TB/s; of 520 204, 5.3; of 800 288, 5.8.
 constexpr int PA_PARTS = 1024, PA_FEW_SEGS = 192;
 // More workgroups than two a CU would fit for smaller heads; it pays for 32 elements only.  With 512 / 768: 2 x 4554 tokens of 23 heads of 32
 // 18.9 / 15.9, 10 x (3624 to 7249) of 4 16.8 / 15.5, fp32 8 x 8192 of 32 96.1 / 93.7; heads of 64, 2 x 4554 18.1 / 17.9, 100000 of 8 41.5 / 42.4.
@@ -586,7 +587,9 @@ __global__ __launch_bounds__(PA_JOIN_THREADS) void page_attn_join_kernel(PageAtt
 // 12.7; 32 of 512 9.7 / 12.0, of 1024 15.9 / 12.7; 128 of 512 12.0 / 14.5, of 1024 19.4 / 19.5, of 2048 32.3 / 30.8; 160 of 2048
 // 33.8 / 35.2; 192 36.8 / 42.7; 256 46.5 / 51.6; 512 86.5 / 89.1.  A long sequence among short ones is where whole segments lose,
 // 10 ns a token of the longest one at worst: 512 of 50 to 2000 tokens 57.7 / 54.7, 256 of 100 to 4000 60.1 / 61.0, 192 of 1 to 16000
-// 181 / 129.
+// 181 / 129.  The higher line guards against the latter only: sequences at the bound lose nothing as whole segments behind it either (240 of
+// 1600 to 2100 tokens, token-major, 42.7 / 44.8; of 4096 80.2 / 85.9; 480 of 3000 115.5 / 118.6, of 4096 156.1 / 159.4; 512 of 4096
+// 168.5 / 172.4), and of 1 to 4096 tokens 240 take 56.0 / 56.5, 480 90.4 / 87.6, 512 93.0 / 96.1.
 constexpr int PA_WHOLE_TOKENS = 768;
 // Eight waves a segment where each has a CU of its own, four where two share one.  us, eight / four: 32 segments of 381 tokens 6.5 / 7.5,
 // 240 of 1850 41.5 / 42.7, 2048 of 256 55.1 / 47.7.  (More than eight query heads: the join of eight waves would not fit the LDS.)

@@ -8,7 +8,8 @@
 // workgroup, in LDS: one trip to memory and one scan, where a launch that leaves it in memory for a second one would cost
 // the second launch and the same trip.  A page that is handed out begins with a new token, so the thread that makes that token's
 // slot also writes the table entry and nothing has to be scattered separately.  The time is that chain -- lengths, sum, search,
-// page, store -- 4.2 us with the launch for a token each of 64 sequences, 9.9 for 1.8 M slots (7 MB).
+// page, store -- 4.0 us in a graph for a token each of 64 sequences, 8.9 a call for 1.8 M slots of 700 (7 MB).  Lengths in place and more
+// than one workgroup: a second launch, 5.8 us for 64 sequences and 1024 slots, 7.4 for 16 and 9216.
 #include "lk_common.h"
 #include "lk_pages.h"
 
